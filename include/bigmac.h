@@ -295,6 +295,53 @@ int bigmac_ep_backward_dispatch(bigmac_layer_t *L, const void *x, int32_t T, con
                                 const bigmac_ep_t *ep, void *dx, const bigmac_grads_t *G, int accumulate,
                                 void *saved, void *scratch, size_t scratch_bytes, void *stream);
 
+/* ---- Operators around the layer ---------------------------------------------------------------------------
+ * Calls of their own, without a handle, on the current CUDA device and `stream`; conventions as above (caller-owned
+ * device memory, nothing allocated, no synchronisation, argument errors launch nothing).  They may be captured into
+ * graphs and run on several streams at once: they share no memory but one status word a device.  bigmac_operator_status
+ * synchronises `stream`, returns BIGMAC_ERR_TIMEOUT if a bounded wait of a bigmac_mx4_matmul on this device ran out
+ * since the last call (its outputs are then undefined), and clears the word. */
+int bigmac_operator_status(void *stream);
+
+/* Microscaled 4-bit floating point for serving.  A matrix of `rows` rows and K columns, K a multiple of 32: every
+ * block of 32 columns of a row has one scale byte s, which stands for 2^(s - 127) (255: NaN), and every element a 4-bit
+ * code of sign, two bits of exponent and one of mantissa, which stands for 0 0.5 1 1.5 2 3 4 6 or the negative.
+ *   codes   [rows, K / 2] bytes, column k in the low half of its byte if k is even, else in the high half
+ *   scales  tiles of 128 rows by 128 columns (4 blocks), 512 bytes each, row tiles outermost: the byte of row m and
+ *           block b lies at ((m / 128) ceil(K / 128) + b / 4) 512 + (m % 32) 16 + (m / 32 % 4) 4 + b % 4.  Bytes of
+ *           blocks behind the last of a row must be 0 where a tile has such blocks.
+ * Both 16-byte aligned.  Weights of E experts are E such matrices one after the other, codes [E, rows, K / 2], scales
+ * [E, ceil(rows / 128), ceil(K / 128), 512].
+ * A GROUPED matrix (offsets set) holds the segments of E experts, rows offsets[e] .. offsets[e + 1] - 1 in the
+ * caller's order (the table bigmac_route writes), each segment from a multiple of 128 rows on; rows the
+ * caller's `rows`, at least offsets[E].  A table that is not ascending from 0 to `rows` at most gives undefined
+ * results, but no access outside the buffers. */
+typedef struct {
+    void *codes, *scales;
+    int32_t rows, K;
+    int32_t E;               /* stacked weights or grouped: 1 .. 1024; one matrix: 0 */
+    const int32_t *offsets;  /* [E + 1] device memory: a grouped matrix; NULL: one matrix, or E stacked */
+} bigmac_mx4_t;
+
+/* Bytes of codes and scales of a matrix (E = 0), of E stacked ones (grouped = 0) or of a grouped one. */
+int bigmac_mx4_bytes(int32_t rows, int32_t K, int32_t E, int grouped, size_t *code_bytes, size_t *scale_bytes);
+
+/* Rows of x [x_rows, K] (dtype; rows ld elements apart, ld * element size a multiple of 16) to 4 bits.  The scale of a block is
+ * 2^(floor(log2 m) - 2), m its largest magnitude (not below 2^-127), each element the nearest of the representable
+ * values, ties to the even code, magnitudes above 6 scales to 6.  A block that holds an infinity or a NaN gets the scale NaN.
+ * Row i of `out` is row i of x or, with slot_of_row (device, [rows]), row slot_of_row[i] / k, zeros where that is
+ * no row of x: the dispatch of the routing tables.  x_rows is out->rows without slot_of_row. */
+int bigmac_mx4_quantize(const void *x, int32_t dtype, int32_t x_rows, int64_t ld, const int32_t *slot_of_row, int32_t k,
+                        const bigmac_mx4_t *out, void *stream);
+/* The numbers that q stands for, y [rows, K] (rows ld elements apart, as above); exact in both dtypes but for
+ * overflow.  Grouped: in the caller's order; rows in no segment are left as they are. */
+int bigmac_mx4_dequantize(const bigmac_mx4_t *q, void *y, int32_t dtype, int64_t ld, void *stream);
+/* c [rows, N] = act(a w^T), act a bigmac_act_t, products and sums in fp32 on the tensor cores, rounded once to dtype; w one
+ * matrix of N = w->rows rows, or, for a grouped a, the a->E = w->E matrices of its experts.  c has a->rows rows in
+ * the caller's order, ldc elements apart; rows in no segment are left as they are. */
+int bigmac_mx4_matmul(const bigmac_mx4_t *a, const bigmac_mx4_t *w, int32_t act, int32_t dtype, void *c, int64_t ldc,
+                      void *stream);
+
 /* bigmac_route for callers that cannot provide scratch memory.  (The paper has no counterpart: this is
  * a deployment variant of the routing step, not part of the method.)
  *

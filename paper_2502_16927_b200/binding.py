@@ -9,7 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
-from typing import Dict, Optional
+from typing import Dict, NamedTuple, Optional
 
 import torch
 
@@ -65,6 +65,12 @@ class bigmac_ep_t(C.Structure):
                [(n, C.c_void_p * BIGMAC_EP_MAX_RANKS) for n in ("xg", "u", "du", "dxg")]
 
 
+
+
+class bigmac_mx4_t(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("scales", C.c_void_p)] + [(n, C.c_int32) for n in ("rows", "K", "E")] + [("offsets", C.c_void_p)]
+
+
 _lib: Optional[C.CDLL] = None
 
 
@@ -111,6 +117,14 @@ def lib() -> C.CDLL:
         L.bigmac_ep_backward_combine.argtypes = [vp, vp, i32, W, EP, G, C.c_int, vp, vp, sz, vp]
         L.bigmac_ep_backward_experts.argtypes = [vp, W, EP, G, C.c_int, vp, vp, sz, vp]
         L.bigmac_ep_backward_dispatch.argtypes = [vp, vp, i32, W, EP, vp, G, C.c_int, vp, vp, sz, vp]
+        Q, i64 = C.POINTER(bigmac_mx4_t), C.c_int64
+        L.bigmac_operator_status.argtypes = [vp]
+        L.bigmac_mx4_bytes.argtypes = [i32, i32, i32, C.c_int, C.POINTER(sz), C.POINTER(sz)]
+        L.bigmac_mx4_quantize.argtypes = [vp, i32, i32, i64, vp, i32, Q, vp]
+        L.bigmac_mx4_dequantize.argtypes = [Q, vp, i32, i64, vp]
+        L.bigmac_mx4_matmul.argtypes = [Q, Q, i32, i32, vp, i64, vp]
+        for name in ("bigmac_operator_status", "bigmac_mx4_bytes", "bigmac_mx4_quantize", "bigmac_mx4_dequantize", "bigmac_mx4_matmul"):
+            getattr(L, name).restype = C.c_int
         for name in ("bigmac_ep_buffer_bytes", "bigmac_ep_workspace_bytes", "bigmac_ep_route", "bigmac_ep_dispatch",
                      "bigmac_ep_experts", "bigmac_ep_combine", "bigmac_ep_backward_combine", "bigmac_ep_backward_experts",
                      "bigmac_ep_backward_dispatch"):
@@ -322,6 +336,118 @@ def bigmac_ep_backward_dispatch(handle, x, T, W, ep, dx, G, accumulate, saved, s
     _check(lib().bigmac_ep_backward_dispatch(handle, _ptr(x), T, C.byref(_weights(W)), C.byref(ep), _ptr(dx),
                                              C.byref(_grads(G)), int(accumulate), _ptr(saved), _ptr(scratch),
                                              _nbytes(scratch), _stream()), "bigmac_ep_backward_dispatch")
+
+
+# ---- operators around the layer ----------------------------------------------------------------------------
+
+def operator_status() -> int:
+    """Synchronises the current stream; 0, or the error that a kernel of the calls below recorded since the last look."""
+    return lib().bigmac_operator_status(_stream())
+
+
+class Mx4(NamedTuple):
+    """A matrix in microscaled 4-bit floating point (bigmac_mx4_t): codes [rows, K / 2] and scales [row tiles, K tiles, 512] of one
+    matrix, both with a leading E for the stacked weights of E experts; with `offsets` the segments of a routing's experts, `rows`
+    rows in the caller's order."""
+    codes: torch.Tensor
+    scales: torch.Tensor
+    offsets: Optional[torch.Tensor] = None
+    rows: Optional[int] = None
+
+
+def _mx4(q: Mx4) -> bigmac_mx4_t:
+    codes, scales, offsets = q.codes, q.scales, q.offsets
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() not in (2, 3) or scales.dim() != codes.dim() + 1:
+        raise ValueError("Mx4: codes [rows, K / 2] and scales [row tiles, K tiles, 512] of torch.uint8, or both with a leading E")
+    *lead, stored, half = codes.shape
+    if tuple(scales.shape) != (*lead, -(-stored // 128), -(-half // 64), 512):
+        raise ValueError(f"Mx4: codes of shape {tuple(codes.shape)} have scales of shape {(*lead, -(-stored // 128), -(-half // 64), 512)}")
+    rows, E = stored, lead[0] if lead else 0
+    if offsets is not None:
+        if lead or offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 2 or q.rows is None:
+            raise ValueError("a grouped Mx4 has codes of two dimensions, int32 offsets [E + 1] and rows")
+        rows, E = q.rows, offsets.numel() - 1
+        if stored < _mx4_stored(rows, E):
+            raise ValueError(f"Mx4: {rows} rows of {E} experts need {_mx4_stored(rows, E)} rows of codes")
+    _same_device(codes, scales, offsets)
+    return bigmac_mx4_t(_ptr(codes), _ptr(scales), rows, 2 * half, E, _ptr(offsets))
+
+
+def _mx4_stored(rows: int, E: int) -> int:
+    """Rows that a grouped matrix has room for: each expert's segment begins at a multiple of 128."""
+    return (rows + min(rows, E) * 127) // 128 * 128
+
+
+def _same_device(*tensors) -> None:
+    """The kernels run on the current device: a tensor of another one would be read through its address there."""
+    here = _current_device() if _current_device is not None else torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != here:
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{here}")
+
+
+_DTYPES = {torch.float32: BIGMAC_F32, torch.bfloat16: BIGMAC_BF16}
+
+
+def _dtype(t: torch.dtype) -> int:
+    try:
+        return _DTYPES[t]
+    except KeyError:
+        raise ValueError(f"{t}: float32 and bfloat16 are supported") from None
+
+
+def _rows_of(t: torch.Tensor, name: str):
+    """(address, row stride) of a matrix whose rows are dense."""
+    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+        raise ValueError(f"{name}: a CUDA matrix with dense rows that do not overlap is needed")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def mx4_quantize(x: torch.Tensor, offsets: Optional[torch.Tensor] = None, slot_of_row: Optional[torch.Tensor] = None, k: int = 1) -> Mx4:
+    """Rows of x to 4 bits (bigmac_mx4_quantize).  With `offsets` (int32 [E + 1], of a routing) grouped by expert; with `slot_of_row`
+    row i is x[slot_of_row[i] // k]: the dispatch."""
+    ptr, ld = _rows_of(x, "x")
+    for name, t in (("offsets", offsets), ("slot_of_row", slot_of_row)):
+        if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or not t.is_cuda or not t.is_contiguous()):
+            raise ValueError(f"{name}: a dense int32 CUDA vector is needed")
+    _same_device(x, offsets, slot_of_row)
+    rows, K = x.shape[0] if slot_of_row is None else slot_of_row.numel(), x.shape[1]
+    if K == 0 or K % 32:
+        raise ValueError(f"K = {K}: blocks of 32 columns")
+    E = 0 if offsets is None else offsets.numel() - 1
+    stored = rows if offsets is None else _mx4_stored(rows, E)
+    codes = torch.empty((stored, K // 2), dtype=torch.uint8, device=x.device)
+    scales = torch.empty((-(-stored // 128), -(-K // 128), 512), dtype=torch.uint8, device=x.device)
+    q = bigmac_mx4_t(codes.data_ptr(), scales.data_ptr(), rows, K, E, None if offsets is None else offsets.data_ptr())
+    _check(lib().bigmac_mx4_quantize(ptr, _dtype(x.dtype), x.shape[0], ld, None if slot_of_row is None else slot_of_row.data_ptr(), k, C.byref(q),
+                                     _stream()), "bigmac_mx4_quantize")
+    return Mx4(codes, scales, offsets, rows)
+
+
+def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The numbers a matrix stands for, in the caller's order of rows.  Of a grouped one, rows in no segment keep what `out` holds."""
+    c = _mx4(q)
+    if out is None:
+        out = torch.empty((c.rows, c.K), dtype=dtype, device=q.codes.device)
+    elif tuple(out.shape) != (c.rows, c.K):
+        raise ValueError(f"out has shape {tuple(out.shape)}, not {(c.rows, c.K)}")
+    ptr, ld = _rows_of(out, "out")
+    _same_device(out)
+    _check(lib().bigmac_mx4_dequantize(C.byref(c), ptr, _dtype(out.dtype), ld, _stream()), "bigmac_mx4_dequantize")
+    return out
+
+
+def mx4_matmul(a: Mx4, w: Mx4, act: int = 3, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """act(a w^T) (bigmac_mx4_matmul; act a bigmac_act_t, 3 the identity).  For a grouped `a`, `w` holds the matrices of its experts."""
+    ca, cw = _mx4(a), _mx4(w)
+    if out is None:
+        out = torch.empty((ca.rows, cw.rows), dtype=dtype, device=a.codes.device)
+    elif tuple(out.shape) != (ca.rows, cw.rows):
+        raise ValueError(f"out has shape {tuple(out.shape)}, not {(ca.rows, cw.rows)}")
+    ptr, ld = _rows_of(out, "out")
+    _same_device(out)
+    _check(lib().bigmac_mx4_matmul(C.byref(ca), C.byref(cw), act, _dtype(out.dtype), ptr, ld, _stream()), "bigmac_mx4_matmul")
+    return out
 
 
 # ---- a small convenience wrapper: owns the handle and the workspaces ------------------------------------

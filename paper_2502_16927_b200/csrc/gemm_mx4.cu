@@ -1,0 +1,317 @@
+// Product of two microscaled 4-bit matrices on the tensor cores (layout: mx4.h):
+//
+//   C[m, n] = sigma( sum_k A(m, k) W(n, k) ),   A(m, k) = e2m1 code * 2^(s - 127) of its block of 32, W alike
+//
+// tcgen05.mma kind::mxf4 takes both operands as codes (64 columns an instruction) and multiplies the blocks' scales in; sums are fp32 in
+// tensor memory.  Dense, or grouped: A holds the segments of E experts, W their E matrices, and C the rows in the caller's order.
+//
+// Persistent CTAs walk the 128 x BN tiles of C.  Warp 0 streams slices of 256 columns into a ring of stages: codes by TMA (128 bytes a
+// row, 128-byte swizzle), scale bytes by bulk copies (512 bytes for 128 rows and 128 columns).  Warp 1 moves a slice's scale
+// bytes to tensor memory (tcgen05.cp, in order before the products that read them, as the products before it are in order before the
+// copy: one buffer is enough) and issues the products.  The other warps drain a finished accumulator while the next one fills.
+#include "tc_common.cuh"
+#include "mx4.h"
+
+namespace bigmac {
+
+using namespace tc;
+
+namespace {
+
+constexpr int kSliceK = 256;                               // columns of a stage: one 128-byte row of codes
+constexpr uint32_t kABytes = 128 * 128;
+constexpr uint32_t kSfTile = 512;
+constexpr int kEpi = 16;                                   // epilogue warps, four to a lane quadrant
+constexpr int kThreadsMx4 = (2 + kEpi) * 32;
+
+struct Mx4Params {
+    void* C;
+    int64_t ldc;
+    const uint8_t *sa, *sw;                                // scale bytes
+    const int32_t* offsets;                                // grouped: the caller's table
+    int M, N, K, E;
+    int64_t capacity;                                      // rows that A has room for (grouped)
+    int act, out_f32;
+    int* status;
+};
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+// 512 bytes of scales, 32 rows of 16 bytes, to four columns of tensor memory in all four lane quadrants.
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+// Without swizzle: groups of 8 rows of 16 bytes, 128 bytes apart.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+}
+__device__ __forceinline__ void umma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
+}
+// Instruction descriptor: e2m1 x e2m1, scales ue8m0, M 128, N bn; `half`: which two of a column's four scale bytes.
+__host__ __device__ constexpr uint32_t instr_desc_mx4(int bn, int half) {
+    return ((uint32_t)(2 * half) << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(bn >> 3) << 17) | (1u << 23) | ((uint32_t)(128 >> 4) << 24) |
+           ((uint32_t)(2 * half) << 29);
+}
+
+struct Mx4Tile {
+    int a_row;                                             // first row in A's storage
+    int n0, expert;
+    int c_row, rows;                                       // first row in C, rows of this tile that exist
+};
+
+// Tile t: all columns of a row tile after each other (its codes stay in L2).
+__device__ __forceinline__ Mx4Tile mx4_tile(const Mx4Params& p, const int32_t* prefix, int BN, int t, int tiles_n) {
+    Mx4Tile q;
+    const int mt = t / tiles_n;
+    q.n0 = (t - mt * tiles_n) * BN;
+    q.a_row = mt * kMx4Tile;
+    if (p.offsets) {
+        q.expert = mx4_find(prefix, p.E, mt);
+        const Mx4Segment s = mx4_segment(p.offsets, q.expert, p.M);
+        const int at = (mt - prefix[q.expert]) * kMx4Tile;
+        q.c_row = s.first + at;
+        q.rows = min(kMx4Tile, s.count - at);
+    } else {
+        q.expert = 0;
+        q.c_row = q.a_row;
+        q.rows = min(kMx4Tile, p.M - q.a_row);
+    }
+    return q;
+}
+
+template <int BN, int STAGES>
+struct Mx4Smem {
+    static constexpr uint32_t kBBytes = BN * 128;
+    static constexpr int kWTiles = BN > 128 ? BN / 128 : 1;              // row tiles of W's scale bytes
+    static constexpr uint32_t kSfBytes = 2 * kSfTile * (1 + kWTiles);    // A's two k tiles, then W's
+    static constexpr uint32_t kStage = kABytes + kBBytes + kSfBytes;     // a multiple of 1024
+    static_assert(kStage % 1024 == 0, "128-byte swizzle: stages on 1024-byte boundaries");
+    static constexpr uint32_t kBars = (2 * STAGES + 4) * 8 + 16;
+    static size_t bytes(int E) { return 1024 + STAGES * kStage + kBars + (size_t)(E + 1) * 4; }
+};
+
+template <int BN, int STAGES>
+__global__ void __launch_bounds__(kThreadsMx4, 1)
+gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32, const __grid_constant__ CUtensorMap map_w,
+                const Mx4Params p) {
+    using S = Mx4Smem<BN, STAGES>;
+    constexpr uint32_t kAcc = BN > 128 ? 1 : 2;                          // accumulators
+    constexpr uint32_t kSfCol = kAcc * BN;                               // scale bytes behind them: A's 8 columns, then W's
+    constexpr uint32_t kTmemCols = kSfCol + 8 + 8 * S::kWTiles <= 256 ? 256 : 512;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
+    uint64_t* full_bar = (uint64_t*)(smem + STAGES * S::kStage);
+    uint64_t* empty_bar = full_bar + STAGES;
+    uint64_t* tmem_full_bar = empty_bar + STAGES;                        // [2]
+    uint64_t* tmem_empty_bar = tmem_full_bar + 2;                        // [2]
+    uint32_t* tmem_slot = (uint32_t*)(tmem_empty_bar + 2);
+    volatile int* dead = (volatile int*)(tmem_slot + 1);
+    int32_t* prefix = (int32_t*)(tmem_slot + 4);                         // [E + 1]
+
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 32) {
+        prefetch_tensormap(&map_a);
+        prefetch_tensormap(&map_a32);
+        prefetch_tensormap(&map_w);
+    }
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&tmem_full_bar[s], 1); mbar_init(&tmem_empty_bar[s], kEpi); }
+        *dead = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc(tmem_slot, kTmemCols);
+    tc_fence_before();
+    __syncthreads();
+    grid_dependency_launch();
+    grid_dependency_wait();
+    if (p.offsets) {
+        if (warp == 2) mx4_tile_prefix(p.offsets, p.E, p.M, prefix);
+        __syncthreads();
+    }
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const int ktiles = mx4_ktiles(p.K), num_kb = (p.K + kSliceK - 1) / kSliceK;
+    const int tiles_n = (p.N + BN - 1) / BN;
+    const int tiles_m = p.offsets ? (int)min((int64_t)prefix[p.E], p.capacity / kMx4Tile) : (p.M + kMx4Tile - 1) / kMx4Tile;
+    const int total = tiles_m * tiles_n;
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ producer
+        if (elect_one()) {
+            const int w_row_tiles = (p.N + 127) / 128;
+            uint32_t s = 0, phase = 1;
+            for (int t = blockIdx.x; t < total; t += gridDim.x) {
+                const Mx4Tile q = mx4_tile(p, prefix, BN, t, tiles_n);
+                const uint8_t* sa = p.sa + (int64_t)(q.a_row / 128) * ktiles * kSfTile;
+                const int wt = q.n0 / 128;
+                const uint8_t* sw = p.sw + ((int64_t)q.expert * w_row_tiles + wt) * ktiles * kSfTile;
+                const int w_tiles = min(S::kWTiles, w_row_tiles - wt);
+                const int boxes = q.rows > 96 ? 0 : (q.rows + 31) / 32;  // of 32 rows; 0: all 128 in one
+                const uint32_t a_bytes = boxes ? boxes * 32 * 128 : kABytes;
+                for (int kb = 0; kb < num_kb; ++kb, s = (s + 1 == STAGES ? 0 : s + 1), phase ^= (s == 0)) {
+                    mbar_wait_lean(&empty_bar[s], phase, dead, p.status);
+                    const uint32_t sf = kSfTile * min(2, ktiles - 2 * kb);
+                    mbar_expect_tx(&full_bar[s], a_bytes + S::kBBytes + sf * (1 + w_tiles));
+                    uint8_t* a = smem + s * S::kStage;
+                    uint8_t* b = a + kABytes;
+                    uint8_t* f = b + S::kBBytes;
+                    if (boxes) for (int i = 0; i < boxes; ++i) tma_load_2d(a + i * 32 * 128, &map_a32, &full_bar[s], kb * 128, q.a_row + 32 * i);
+                    else tma_load_2d(a, &map_a, &full_bar[s], kb * 128, q.a_row);
+                    tma_load_2d(b, &map_w, &full_bar[s], kb * 128, q.expert * p.N + q.n0);
+                    bulk_load(f, sa + kb * 2 * kSfTile, sf, &full_bar[s]);
+                    for (int i = 0; i < w_tiles; ++i)
+                        bulk_load(f + 2 * kSfTile * (1 + i), sw + ((int64_t)i * ktiles + kb * 2) * kSfTile, sf, &full_bar[s]);
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ scale bytes and products, one thread
+        if (elect_one()) {
+            const uint64_t da0 = smem_desc(smem_u32(smem), 16, 1024), db0 = smem_desc(smem_u32(smem + kABytes), 16, 1024);
+            const uint64_t df0 = scale_desc(smem_u32(smem + kABytes + S::kBBytes));
+            uint32_t stage = 0, phase = 0, local = 0;
+            for (int t = blockIdx.x; t < total; t += gridDim.x, ++local) {
+                const uint32_t acc = kAcc == 2 ? local & 1 : 0, use = kAcc == 2 ? local >> 1 : local;
+                // a 64-column tile in the second half of W's row tile: its rows' bytes start two columns further
+                const uint32_t shift = BN == 64 ? (uint32_t)((t % tiles_n) & 1) * 2 : 0;
+                mbar_wait_lean(&tmem_empty_bar[acc], (use & 1) ^ 1, dead, p.status);
+                tc_fence_after();
+                const uint32_t d = tmem + acc * BN, fa = tmem + kSfCol, fw = fa + 8;
+                for (int kb = 0; kb < num_kb; ++kb) {
+                    mbar_wait_lean(&full_bar[stage], phase, dead, p.status);
+                    tc_fence_after();
+                    const uint64_t step = (uint64_t)stage * (S::kStage >> 4);
+                    const uint64_t da = da0 + step, db = db0 + step, df = df0 + step;
+                    const int cols = min(kSliceK, p.K - kb * kSliceK);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        if (j * 128 >= cols) break;
+                        copy_scales(fa + 4 * j, df + j * (kSfTile >> 4));
+#pragma unroll
+                        for (int i = 0; i < S::kWTiles; ++i)
+                            copy_scales(fw + 4 * (j * S::kWTiles + i), df + ((2 * (1 + i) + j) * (kSfTile >> 4)));
+                    }
+#pragma unroll
+                    for (int kk = 0; kk < kSliceK / 64; ++kk) {
+                        if (kk * 64 >= cols) break;
+                        umma_mx4(d, da + kk * 2, db + kk * 2, instr_desc_mx4(BN, kk & 1), fa + 4 * (kk >> 1), fw + 4 * S::kWTiles * (kk >> 1) + shift,
+                                 kb != 0 || kk != 0);
+                    }
+                    umma_commit(&empty_bar[stage]);
+                    if (++stage == STAGES) { stage = 0; phase ^= 1; }
+                }
+                umma_commit(&tmem_full_bar[acc]);
+            }
+        }
+    } else {
+        // ------------------------------------------------------------------ epilogue
+        const int quad = warp & 3, part = (warp - 2) >> 2;
+        constexpr int kChunks = BN / 32, kPerWarp = (kChunks + 3) / 4;   // chunks of 32 columns: part, part + 4, ...
+        uint32_t local = 0;
+        const int esz = p.out_f32 ? 4 : 2;
+        const bool vec_ok = (p.ldc * esz) % 32 == 0 && (uintptr_t)p.C % 32 == 0;
+        for (int t = blockIdx.x; t < total; t += gridDim.x, ++local) {
+            const Mx4Tile q = mx4_tile(p, prefix, BN, t, tiles_n);
+            const uint32_t acc = kAcc == 2 ? local & 1 : 0, use = kAcc == 2 ? local >> 1 : local;
+            mbar_wait_lean(&tmem_full_bar[acc], use & 1, dead, p.status);
+            tc_fence_after();
+            const int row = quad * 32 + lane;
+            const bool row_ok = row < q.rows;
+            const uint32_t t_addr = tmem + acc * BN + ((uint32_t)(quad * 32) << 16);
+#pragma unroll
+            for (int c = 0; c < kPerWarp; ++c) {
+                const int chunk = part + 4 * c;
+                float v[32];
+                const bool have = chunk < kChunks;
+                if (have) { tmem_load_32_nowait(t_addr + chunk * 32, (uint32_t*)v); tmem_load_wait(); }
+                if (c == kPerWarp - 1) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&tmem_empty_bar[acc]);
+                }
+                const int col0 = q.n0 + chunk * 32;
+                if (!have || col0 >= p.N || !row_ok) continue;
+                if (p.act != BIGMAC_ACT_IDENTITY) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] = act_apply(p.act, v[i]);
+                }
+                const int64_t off = (int64_t)(q.c_row + row) * p.ldc + col0;
+                if (vec_ok && col0 + 32 <= p.N) {
+                    if (p.out_f32) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) st_global_32B((float*)p.C + off + 8 * i, (const uint32_t*)v + 8 * i);
+                    } else {
+                        uint32_t w[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+                        st_global_32B((__nv_bfloat16*)p.C + off, w);
+                        st_global_32B((__nv_bfloat16*)p.C + off + 16, w + 8);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        if (col0 + i >= p.N) break;
+                        if (p.out_f32) ((float*)p.C)[off + i] = v[i];
+                        else ((__nv_bfloat16*)p.C)[off + i] = __float2bfloat16(v[i]);
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+template <int BN, int STAGES>
+cudaError_t launch(const Mx4View& a, const Mx4View& w, const Mx4Params& p, int64_t max_tiles_m, cudaStream_t stream) {
+    CUtensorMap ma, ma32, mw;
+    const uint64_t row = (uint64_t)p.K / 2;
+    const uint64_t a_rows = a.offsets ? (uint64_t)a.capacity : (uint64_t)a.rows, w_rows = (uint64_t)w.rows * (w.E > 0 ? w.E : 1);
+    if (!make_map_u8(&ma, a.codes, row, a_rows, row, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map_u8(&ma32, a.codes, row, a_rows, row, 128, 32, CU_TENSOR_MAP_SWIZZLE_128B) ||
+        !make_map_u8(&mw, w.codes, row, w_rows, row, 128, BN, CU_TENSOR_MAP_SWIZZLE_128B))
+        return cudaErrorInvalidValue;
+    static PerDeviceOnce once;
+    auto kernel = gemm_mx4_kernel<BN, STAGES>;
+    using S = Mx4Smem<BN, STAGES>;
+    static_assert(1024 + STAGES * S::kStage + S::kBars + (kMaxExperts + 1) * 4 <= 227 * 1024, "shared memory of a block");
+    int dev;
+    if (once.needed(&dev)) {
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::bytes(kMaxExperts));
+        if (e != cudaSuccess) return e;
+        once.mark(dev);
+    }
+    const int64_t tiles = max_tiles_m * ((p.N + BN - 1) / BN);
+    const int sms = gemm_tc_sm_count();
+    return launch_chained(kernel, (int)(tiles < sms ? tiles : sms), kThreadsMx4, S::bytes(p.offsets ? p.E : 0), stream, ma, ma32, mw, p);
+}
+
+}  // namespace
+
+cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int dtype, void* c, int64_t ldc, int* status, cudaStream_t stream) {
+    if (a.rows == 0 || w.rows == 0) return cudaSuccess;
+    Mx4Params p{};
+    p.C = c; p.ldc = ldc; p.sa = a.scales; p.sw = w.scales; p.offsets = a.offsets;
+    p.M = a.rows; p.N = w.rows; p.K = a.K; p.E = a.E; p.capacity = a.capacity;
+    p.act = act; p.out_f32 = dtype == BIGMAC_F32; p.status = status;
+    const int64_t tiles_m = a.offsets ? a.capacity / kMx4Tile : (a.rows + kMx4Tile - 1) / kMx4Tile;
+    const int sms = gemm_tc_sm_count();
+    if (tiles_m * ((p.N + 127) / 128) <= sms) return launch<64, 6>(a, w, p, tiles_m, stream);
+    return launch<128, 6>(a, w, p, tiles_m, stream);
+}
+
+}  // namespace bigmac

@@ -1,0 +1,70 @@
+// Shared by the units that work on microscaled 4-bit matrices: the layout of a matrix and of the segments of a grouped one.
+//
+// A matrix of `rows` rows and K columns (K a multiple of 32): element (m, k) is a 4-bit float (e2m1) in nibble k % 2 of byte k / 2
+// of row m, times 2^(s - 127) with s the scale byte of its block of 32 columns.  Scale bytes lie as tcgen05.cp moves them to tensor memory, in tiles of
+// 128 rows by 4 blocks (128 columns): tile (m / 128, k / 128) is 512 consecutive bytes, in it byte (m % 32) 16 + (m / 32 % 4) 4 +
+// (k / 32 % 4); tiles of one row tile follow each other.
+// A grouped matrix holds the segments of E experts, each from a multiple of 128 rows on.
+#pragma once
+#include "internal.h"
+
+namespace bigmac {
+
+constexpr int kMx4Tile = 128;
+
+__host__ __device__ inline int mx4_ktiles(int K) { return (K + 127) / 128; }
+__host__ __device__ inline int64_t mx4_scale_at(int64_t row, int block, int ktiles) {
+    return ((row >> 7) * ktiles + (block >> 2)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (block & 3);
+}
+// Rows a grouped matrix has room for: every expert may fill its last 128 rows with one row only.
+inline int64_t mx4_padded_rows(int64_t rows, int E) {
+    const int64_t ragged = rows < E ? rows : E;
+    return (rows + ragged * (kMx4Tile - 1)) / kMx4Tile * kMx4Tile;
+}
+
+#ifdef __CUDACC__
+// Rows of expert e by the caller's table, as far as they lie in [0, rows): a table that is none reads and writes nothing outside.
+struct Mx4Segment { int first, count; };
+__device__ __forceinline__ Mx4Segment mx4_segment(const int32_t* __restrict__ offsets, int e, int rows) {
+    const int a = min(max(offsets[e], 0), rows), b = min(max(offsets[e + 1], a), rows);
+    return {a, b - a};
+}
+// out[e] = tiles of the experts before e, e = 0 .. E; all threads of a warp.
+__device__ __forceinline__ void mx4_tile_prefix(const int32_t* __restrict__ offsets, int E, int rows, int32_t* out) {
+    const int lane = threadIdx.x & 31, per = (E + 31) / 32, e0 = min(E, lane * per), e1 = min(E, e0 + per);
+    int mine = 0;
+    for (int e = e0; e < e1; ++e) mine += (mx4_segment(offsets, e, rows).count + kMx4Tile - 1) / kMx4Tile;
+    int run = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int a = __shfl_up_sync(0xffffffffu, run, o);
+        if (lane >= o) run += a;
+    }
+    if (lane == 31) out[E] = run;
+    run -= mine;
+    for (int e = e0; e < e1; ++e) { out[e] = run; run += (mx4_segment(offsets, e, rows).count + kMx4Tile - 1) / kMx4Tile; }
+}
+// The last e in [0, E) with table[e] <= v; table ascending, table[0] <= v.
+__device__ __forceinline__ int mx4_find(const int32_t* table, int E, int v) {
+    int lo = 0, hi = E - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (table[mid] <= v) lo = mid; else hi = mid - 1;
+    }
+    return lo;
+}
+#endif
+
+struct Mx4View {                      // one matrix, or E stacked ones (weights), or the segments of E experts (offsets set)
+    uint8_t *codes, *scales;
+    int rows, K, E;                   // rows of the caller's order (of one matrix, where E are stacked)
+    const int32_t* offsets;
+    int64_t capacity;                 // rows that `codes` and `scales` have room for
+};
+
+cudaError_t launch_mx4_quantize(const void* x, int dtype, int64_t ld, const int32_t* slot_of_row, int k, int x_rows, const Mx4View& out,
+                                cudaStream_t stream);
+cudaError_t launch_mx4_dequantize(const Mx4View& q, void* y, int dtype, int64_t ld, cudaStream_t stream);
+cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int dtype, void* c, int64_t ldc, int* status, cudaStream_t stream);
+
+}  // namespace bigmac

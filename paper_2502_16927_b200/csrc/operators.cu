@@ -1,0 +1,98 @@
+// C-ABI entry points of the operators around the layer: argument checks and launches.
+#include "bigmac.h"
+#include "internal.h"
+#include "mx4.h"
+
+using namespace bigmac;
+
+static __device__ int g_operator_status;
+
+namespace {
+
+inline bool is_aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+inline bool dtype_ok(int32_t dtype) { return dtype == BIGMAC_F32 || dtype == BIGMAC_BF16; }
+inline int64_t esize_of(int32_t dtype) { return dtype == BIGMAC_BF16 ? 2 : 4; }
+
+// Device address of the status word, resolved once per device.
+int* status_word() {
+    static int* cached[64] = {};
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return nullptr;
+    if (!cached[dev]) {
+        void* p = nullptr;
+        if (cudaGetSymbolAddress(&p, g_operator_status) != cudaSuccess) { cudaGetLastError(); return nullptr; }
+        cached[dev] = (int*)p;
+    }
+    return cached[dev];
+}
+
+int check_mx4(const bigmac_mx4_t* q, bool stacked_allowed) {
+    if (!q || q->rows < 0 || q->K <= 0 || q->E < 0 || q->E > kMaxExperts || (q->offsets && q->E == 0)) return BIGMAC_ERR_INVALID_ARG;
+    if (q->K % 32 != 0 || q->K > (1 << 20)) return BIGMAC_ERR_UNSUPPORTED;
+    if (q->E > 0 && !q->offsets && !stacked_allowed) return BIGMAC_ERR_INVALID_ARG;
+    if (!is_aligned(q->codes, 16) || !is_aligned(q->scales, 16) || !is_aligned(q->offsets, 4)) return BIGMAC_ERR_INVALID_ARG;
+    const int64_t rows = q->offsets ? mx4_padded_rows(q->rows, q->E) : (int64_t)q->rows * (q->E > 0 ? q->E : 1);
+    if (rows > (int64_t)0x7fffff00) return BIGMAC_ERR_UNSUPPORTED;       // row numbers are 32-bit
+    if (rows > 0 && (!q->codes || !q->scales)) return BIGMAC_ERR_INVALID_ARG;
+    return BIGMAC_OK;
+}
+Mx4View view_of(const bigmac_mx4_t* q) {
+    const int64_t capacity = q->offsets ? mx4_padded_rows(q->rows, q->E) : q->rows;
+    return Mx4View{(uint8_t*)q->codes, (uint8_t*)q->scales, q->rows, q->K, q->E, q->offsets, capacity};
+}
+
+}  // namespace
+
+extern "C" {
+
+int bigmac_operator_status(void* stream) {
+    int* at = status_word();
+    if (!at) return BIGMAC_ERR_CUDA;
+    cudaStream_t st = (cudaStream_t)stream;
+    int word = 0;
+    if (cudaMemcpyAsync(&word, at, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaMemsetAsync(at, 0, sizeof(int), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
+        return BIGMAC_ERR_CUDA;
+    return word == 0 ? BIGMAC_OK : BIGMAC_ERR_TIMEOUT;
+}
+
+int bigmac_mx4_bytes(int32_t rows, int32_t K, int32_t E, int grouped, size_t* code_bytes, size_t* scale_bytes) {
+    if (rows < 0 || K <= 0 || E < 0 || E > kMaxExperts || (grouped && E == 0) || !code_bytes || !scale_bytes) return BIGMAC_ERR_INVALID_ARG;
+    if (K % 32 != 0 || K > (1 << 20)) return BIGMAC_ERR_UNSUPPORTED;
+    const int64_t one = grouped ? mx4_padded_rows(rows, E) : rows, many = grouped || E == 0 ? 1 : E;
+    *code_bytes = (size_t)(one * many) * (K / 2);
+    *scale_bytes = (size_t)((one + kMx4Tile - 1) / kMx4Tile * many) * mx4_ktiles(K) * 512;
+    return BIGMAC_OK;
+}
+
+int bigmac_mx4_quantize(const void* x, int32_t dtype, int32_t x_rows, int64_t ld, const int32_t* slot_of_row, int32_t k, const bigmac_mx4_t* out,
+                        void* stream) {
+    const int s = check_mx4(out, false);
+    if (s != BIGMAC_OK) return s;
+    if (!dtype_ok(dtype) || x_rows < 0 || ld < out->K || (ld * esize_of(dtype)) % 16 || !is_aligned(x, 16) || !is_aligned(slot_of_row, 4) ||
+        (slot_of_row ? k < 1 : x_rows != out->rows) || (x_rows > 0 && !x))
+        return BIGMAC_ERR_INVALID_ARG;
+    return launch_mx4_quantize(x, dtype, ld, slot_of_row, k, x_rows, view_of(out), (cudaStream_t)stream) == cudaSuccess ? BIGMAC_OK : BIGMAC_ERR_CUDA;
+}
+
+int bigmac_mx4_dequantize(const bigmac_mx4_t* q, void* y, int32_t dtype, int64_t ld, void* stream) {
+    const int s = check_mx4(q, false);
+    if (s != BIGMAC_OK) return s;
+    if (!dtype_ok(dtype) || ld < q->K || (ld * esize_of(dtype)) % 16 || !is_aligned(y, 16) || (q->rows > 0 && !y)) return BIGMAC_ERR_INVALID_ARG;
+    return launch_mx4_dequantize(view_of(q), y, dtype, ld, (cudaStream_t)stream) == cudaSuccess ? BIGMAC_OK : BIGMAC_ERR_CUDA;
+}
+
+int bigmac_mx4_matmul(const bigmac_mx4_t* a, const bigmac_mx4_t* w, int32_t act, int32_t dtype, void* c, int64_t ldc, void* stream) {
+    int s = check_mx4(a, false);
+    if (s == BIGMAC_OK) s = check_mx4(w, true);
+    if (s != BIGMAC_OK) return s;
+    if (!dtype_ok(dtype) || act < 0 || act > BIGMAC_ACT_IDENTITY || w->offsets || a->K != w->K || a->E != w->E || ldc < w->rows || !is_aligned(c, 16))
+        return BIGMAC_ERR_INVALID_ARG;
+    if (a->rows == 0 || w->rows == 0) return BIGMAC_OK;
+    if (!c) return BIGMAC_ERR_INVALID_ARG;
+    int* status = status_word();
+    if (!status) return BIGMAC_ERR_CUDA;
+    return launch_mx4_matmul(view_of(a), view_of(w), act, dtype, c, ldc, status, (cudaStream_t)stream) == cudaSuccess ? BIGMAC_OK : BIGMAC_ERR_CUDA;
+}
+
+}  // extern "C"
