@@ -303,6 +303,49 @@ int bigmac_ep_backward_dispatch(bigmac_layer_t *L, const void *x, int32_t T, con
  * since the last call (its outputs are then undefined), and clears the word. */
 int bigmac_operator_status(void *stream);
 
+/* The joint of two blocks of a network: what is between one block's output y and the next block's input n.
+ *
+ *     r = rho x + gate * N_post(y)          the residual stream after the block
+ *     n = N_pre(r)                          what the next block reads
+ *
+ * N(v) = (v - mean) / sqrt(var + eps) * w + b over the d columns of a row (BIGMAC_NORM_LAYER), v / sqrt(mean(v^2) + eps) * w
+ * + b (BIGMAC_NORM_RMS), or v * w + b (BIGMAC_NORM_NONE, post only); w = 1 and b = 0 where the vector is NULL.  y = NULL: r = rho x (the
+ * norm before a first block); n = NULL with pre_kind NONE: no norm follows.  One call reads every tensor once and
+ * computes in fp32; n is the norm of r before r is rounded.  The gate is one factor a row (fp32 [T]), a vector of parameters
+ * (fp32 [d]) or a factor for every element ([T, d], dtype).
+ * Matrices are [T, d] of dtype with rows `ld` elements apart; parameters, their gradients, row gates and stats are fp32.  Pointers
+ * are aligned to their element type; d a multiple of 8 with every pointer and row on a 16-byte boundary runs on 16-byte accesses, anything
+ * else on single elements.  d <= 8192.  r may be x and n may be y (same pointer and ld), dx may be dr and dy may
+ * be dn; other overlaps of inputs and outputs are errors of the caller. */
+typedef enum { BIGMAC_NORM_NONE = 0, BIGMAC_NORM_RMS = 1, BIGMAC_NORM_LAYER = 2 } bigmac_norm_t;
+typedef enum { BIGMAC_GATE_NONE = 0, BIGMAC_GATE_TOKEN = 1, BIGMAC_GATE_CHANNEL = 2, BIGMAC_GATE_FULL = 3 } bigmac_gate_t;
+typedef struct {
+    void *p;
+    int64_t ld;
+} bigmac_rows_t;
+typedef struct {
+    int32_t d, dtype, post_kind, pre_kind, gate_kind;
+    float post_eps, pre_eps, residual_scale;          /* finite, eps >= 0 */
+    const float *w_post, *b_post, *w_pre, *b_pre;     /* [d] or NULL */
+    bigmac_rows_t x, y, gate;                         /* gate.ld of BIGMAC_GATE_FULL only */
+    bigmac_rows_t r, n;                               /* forward; r may be NULL */
+    float *stats;                                     /* [T, 4], 16-byte aligned: written by a forward that gets it (else NULL),
+                                                         read by the backward */
+    /* backward only */
+    bigmac_rows_t dr, dn;                             /* gradients of r and n; one of them may be NULL */
+    bigmac_rows_t dx, dy, dgate;                      /* NULL: not wanted; dgate of the gate's shape and type */
+    float *dw_post, *db_post, *dw_pre, *db_pre;       /* [d] or NULL */
+} bigmac_residual_norm_t;
+
+int bigmac_residual_norm_forward(const bigmac_residual_norm_t *q, int32_t T, void *stream);
+/* Scratch of the backward (16-byte aligned; none is needed if no gradient of a vector of parameters is wanted). */
+int bigmac_residual_norm_scratch_bytes(const bigmac_residual_norm_t *q, int32_t T, size_t *scratch_bytes);
+/* Gradients of sum(r dr) + sum(n dn).  x, y, gate, parameters and stats are those of the forward.  accumulate = 1 adds to the
+ * gradients of vectors of parameters (a channel gate's among them), 0 overwrites them; those of rows are
+ * always written.  Sums over rows have a fixed order: a call repeats itself bit for bit. */
+int bigmac_residual_norm_backward(const bigmac_residual_norm_t *q, int32_t T, int accumulate, void *scratch,
+                                  size_t scratch_bytes, void *stream);
+
 /* Microscaled 4-bit floating point for serving.  A matrix of `rows` rows and K columns, K a multiple of 32: every
  * block of 32 columns of a row has one scale byte s, which stands for 2^(s - 127) (255: NaN), and every element a 4-bit
  * code of sign, two bits of exponent and one of mantissa, which stands for 0 0.5 1 1.5 2 3 4 6 or the negative.

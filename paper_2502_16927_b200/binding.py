@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes as C
 import functools
 import os
+import struct
 from typing import Dict, NamedTuple, Optional
 
 import torch
@@ -123,7 +124,11 @@ def lib() -> C.CDLL:
         L.bigmac_mx4_quantize.argtypes = [vp, i32, i32, i64, vp, i32, Q, vp]
         L.bigmac_mx4_dequantize.argtypes = [Q, vp, i32, i64, vp]
         L.bigmac_mx4_matmul.argtypes = [Q, Q, i32, i32, vp, i64, vp]
-        for name in ("bigmac_operator_status", "bigmac_mx4_bytes", "bigmac_mx4_quantize", "bigmac_mx4_dequantize", "bigmac_mx4_matmul"):
+        L.bigmac_residual_norm_forward.argtypes = [vp, i32, vp]
+        L.bigmac_residual_norm_scratch_bytes.argtypes = [vp, i32, C.POINTER(sz)]
+        L.bigmac_residual_norm_backward.argtypes = [vp, i32, C.c_int, vp, sz, vp]
+        for name in ("bigmac_residual_norm_forward", "bigmac_residual_norm_scratch_bytes", "bigmac_residual_norm_backward",
+                     "bigmac_operator_status", "bigmac_mx4_bytes", "bigmac_mx4_quantize", "bigmac_mx4_dequantize", "bigmac_mx4_matmul"):
             getattr(L, name).restype = C.c_int
         for name in ("bigmac_ep_buffer_bytes", "bigmac_ep_workspace_bytes", "bigmac_ep_route", "bigmac_ep_dispatch",
                      "bigmac_ep_experts", "bigmac_ep_combine", "bigmac_ep_backward_combine", "bigmac_ep_backward_experts",
@@ -343,6 +348,123 @@ def bigmac_ep_backward_dispatch(handle, x, T, W, ep, dx, G, accumulate, saved, s
 def operator_status() -> int:
     """Synchronises the current stream; 0, or the error that a kernel of the calls below recorded since the last look."""
     return lib().bigmac_operator_status(_stream())
+
+
+BIGMAC_NORM_NONE, BIGMAC_NORM_RMS, BIGMAC_NORM_LAYER = 0, 1, 2
+BIGMAC_GATE_NONE, BIGMAC_GATE_TOKEN, BIGMAC_GATE_CHANNEL, BIGMAC_GATE_FULL = 0, 1, 2, 3
+
+
+class Norm(NamedTuple):
+    """A norm of the joint (bigmac_norm_t) with its fp32 parameters [d]; None: ones, zeros."""
+    kind: int
+    weight: Optional[torch.Tensor] = None
+    bias: Optional[torch.Tensor] = None
+    eps: float = 1e-6
+
+
+_NO_NORM = Norm(BIGMAC_NORM_NONE)
+# bigmac_residual_norm_t, packed at once: a ctypes structure of as many members takes longer to fill than a token's kernel runs
+_RESIDUAL_NORM = struct.Struct("@5i3f4P" + 5 * "Pq" + "P" + 5 * "Pq" + "4P")
+_NOTHING = (0, 0)
+
+
+def _rows_like(t: Optional[torch.Tensor], name: str, shape, dtype):
+    """(address, row stride) of a [T, d] matrix of the joint, (0, 0) where there is none."""
+    if t is None:
+        return _NOTHING
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: {tuple(shape)} of {dtype} is needed, not {tuple(t.shape)} of {t.dtype}")
+    return _rows_of(t, name)
+
+
+def _vector(t: Optional[torch.Tensor], name: str, n: int) -> int:
+    if t is None:
+        return 0
+    if t.dtype is not torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: a dense fp32 CUDA vector of {n} is needed")
+    return t.data_ptr()
+
+
+def _gate_kind(gate, x, gate_kind) -> int:
+    """The gate's kind by its shape; a vector as long as both T and d is one factor a token unless gate_kind says otherwise."""
+    if gate is None:
+        kind = BIGMAC_GATE_NONE
+    elif gate.dim() == 2:
+        kind = BIGMAC_GATE_FULL
+    elif gate_kind is not None:
+        kind = gate_kind
+    else:
+        kind = BIGMAC_GATE_TOKEN if gate.shape[0] == x.shape[0] else BIGMAC_GATE_CHANNEL
+    if gate_kind is not None and kind != gate_kind:
+        raise ValueError(f"gate_kind {gate_kind}: the gate's shape says {kind}")
+    return kind
+
+
+def _joint(x, y, gate, gate_kind, post, pre, residual_scale):
+    """The members of bigmac_residual_norm_t that forward and backward share, up to `gate`."""
+    if x.dim() != 2:
+        raise ValueError("x: [T, d]")
+    T, d = x.shape
+    at = _rows_of(x, "x")
+    kind = _gate_kind(gate, x, gate_kind)
+    post, pre = post or _NO_NORM, pre or _NO_NORM
+    if kind == BIGMAC_GATE_FULL:
+        g = _rows_like(gate, "gate", x.shape, x.dtype)
+    else:
+        g = (_vector(gate, "gate", T if kind == BIGMAC_GATE_TOKEN else d), 0)
+    _same_device(x, y, gate, post.weight, post.bias, pre.weight, pre.bias)
+    return (d, _dtype(x.dtype), post.kind, pre.kind, kind, post.eps, pre.eps, residual_scale, _vector(post.weight, "post.weight", d),
+            _vector(post.bias, "post.bias", d), _vector(pre.weight, "pre.weight", d), _vector(pre.bias, "pre.bias", d), *at,
+            *_rows_like(y, "y", x.shape, x.dtype), *g), kind
+
+
+def residual_norm_forward(x: torch.Tensor, y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, post: Optional[Norm] = None,
+                          pre: Optional[Norm] = None, residual_scale: float = 1.0, training: bool = False, gate_kind: Optional[int] = None,
+                          r: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None):
+    """r = residual_scale x + gate N_post(y) and n = N_pre(r) (bigmac_residual_norm_forward): (r, n, stats), n None without `pre`, stats (for
+    the backward) None unless `training`.  gate: [T] or [d] fp32, or [T, d].  r and n may be given, in place too (r is x, n is y)."""
+    members, _ = _joint(x, y, gate, gate_kind, post, pre, residual_scale)
+    if r is None:
+        r = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if n is None and pre is not None and pre.kind != BIGMAC_NORM_NONE:
+        n = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    stats = torch.empty((x.shape[0], 4), dtype=torch.float32, device=x.device) if training else None
+    _same_device(r, n)
+    q = _RESIDUAL_NORM.pack(*members, *_rows_like(r, "r", x.shape, x.dtype), *_rows_like(n, "n", x.shape, x.dtype),
+                            0 if stats is None else stats.data_ptr(), *(14 * (0,)))
+    _check(lib().bigmac_residual_norm_forward(q, x.shape[0], _stream()), "bigmac_residual_norm_forward")
+    return r, n, stats
+
+
+def residual_norm_backward(x, y, gate, post, pre, dr, dn, stats, G: Optional[Dict[str, torch.Tensor]] = None, residual_scale: float = 1.0,
+                           accumulate: bool = False, gate_kind: Optional[int] = None):
+    """Gradients of sum(r dr) + sum(n dn) (bigmac_residual_norm_backward): (dx, dy, dgate), None for what was not in the call.  G holds
+    fp32 buffers for the gradients of the parameters, any of dw_post, db_post, dw_pre, db_pre and, for a gate [d], dgate (returned,
+    too); with `accumulate` they are added to.  dr or dn may be None."""
+    members, kind = _joint(x, y, gate, gate_kind, post, pre, residual_scale)
+    G, (T, d) = G or {}, x.shape
+    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dy = None if y is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    if kind == BIGMAC_GATE_CHANNEL:
+        dgate = G.get("dgate")
+        dg = (_vector(dgate, "dgate", d), 0)
+    elif kind == BIGMAC_GATE_NONE:
+        dgate, dg = None, _NOTHING
+    else:
+        dgate = torch.empty(gate.shape, dtype=gate.dtype, device=x.device)
+        dg = (dgate.data_ptr(), d)
+    if stats is None or stats.dtype is not torch.float32 or stats.shape != (T, 4) or not stats.is_contiguous():
+        raise ValueError("stats: those of a training forward of the same rows")
+    grads = [_vector(G.get(name), name, d) for name in ("dw_post", "db_post", "dw_pre", "db_pre")]
+    _same_device(dr, dn, stats, *G.values())
+    q = _RESIDUAL_NORM.pack(*members, 0, 0, 0, 0, stats.data_ptr(), *_rows_like(dr, "dr", x.shape, x.dtype), *_rows_like(dn, "dn", x.shape, x.dtype),
+                            dx.data_ptr(), d, *((0, 0) if dy is None else (dy.data_ptr(), d)), *dg, *grads)
+    need = C.c_size_t()
+    _check(lib().bigmac_residual_norm_scratch_bytes(q, T, C.byref(need)), "bigmac_residual_norm_scratch_bytes")
+    scratch = torch.empty(need.value, dtype=torch.uint8, device=x.device) if need.value else None
+    _check(lib().bigmac_residual_norm_backward(q, T, int(accumulate), None if scratch is None else scratch.data_ptr(), need.value, _stream()),
+           "bigmac_residual_norm_backward")
+    return dx, dy, dgate
 
 
 class Mx4(NamedTuple):

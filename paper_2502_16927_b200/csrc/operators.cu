@@ -1,7 +1,10 @@
 // C-ABI entry points of the operators around the layer: argument checks and launches.
+#include <cmath>
+
 #include "bigmac.h"
 #include "internal.h"
 #include "mx4.h"
+#include "residual_norm.h"
 
 using namespace bigmac;
 
@@ -41,9 +44,83 @@ Mx4View view_of(const bigmac_mx4_t* q) {
     return Mx4View{(uint8_t*)q->codes, (uint8_t*)q->scales, q->rows, q->K, q->E, q->offsets, capacity};
 }
 
+// A matrix of the joint: aligned to its elements, rows that do not overlap.  *vec: rows on 16-byte boundaries, too.
+bool rows_ok(const bigmac_rows_t& m, int64_t d, int64_t es, bool* vec) {
+    if (!m.p) return true;
+    if (!is_aligned(m.p, es) || m.ld < d) return false;
+    if (!is_aligned(m.p, 16) || (m.ld * es) % 16) *vec = false;
+    return true;
+}
+bool vector_ok(const void* p, bool* vec) {
+    if (!is_aligned(p, 4)) return false;
+    if (!is_aligned(p, 16)) *vec = false;
+    return true;
+}
+
+int check_residual_norm(const bigmac_residual_norm_t* q, int32_t T, bool backward, ResNorm* a) {
+    if (!q || T < 0 || q->d <= 0 || !dtype_ok(q->dtype) || q->post_kind < 0 || q->post_kind > BIGMAC_NORM_LAYER || q->pre_kind < 0 ||
+        q->pre_kind > BIGMAC_NORM_LAYER || q->gate_kind < 0 || q->gate_kind > BIGMAC_GATE_FULL)
+        return BIGMAC_ERR_INVALID_ARG;
+    if (!(q->post_eps >= 0) || !(q->pre_eps >= 0) || !std::isfinite(q->post_eps) || !std::isfinite(q->pre_eps) || !std::isfinite(q->residual_scale))
+        return BIGMAC_ERR_INVALID_ARG;
+    if (q->d > kResNormMaxWidth) return BIGMAC_ERR_UNSUPPORTED;
+    const int64_t es = esize_of(q->dtype);
+    *a = ResNorm{q, T, q->d % 8 == 0};
+    bool ok = rows_ok(q->x, q->d, es, &a->vec) && rows_ok(q->y, q->d, es, &a->vec) && vector_ok(q->w_post, &a->vec) && vector_ok(q->b_post, &a->vec) &&
+              vector_ok(q->w_pre, &a->vec) && vector_ok(q->b_pre, &a->vec) && is_aligned(q->stats, 16);
+    ok = ok && (q->gate_kind == BIGMAC_GATE_FULL ? rows_ok(q->gate, q->d, es, &a->vec) : vector_ok(q->gate.p, &a->vec));
+    if (!ok) return BIGMAC_ERR_INVALID_ARG;
+    if (q->pre_kind == BIGMAC_NORM_NONE && (q->w_pre || q->b_pre)) return BIGMAC_ERR_INVALID_ARG;
+    if (q->gate_kind == BIGMAC_GATE_NONE && (q->gate.p || q->dgate.p)) return BIGMAC_ERR_INVALID_ARG;
+    if (T == 0) return BIGMAC_OK;                                      // matrices without rows have no address
+    if (q->gate_kind != BIGMAC_GATE_NONE && !q->gate.p) return BIGMAC_ERR_INVALID_ARG;
+    // the norm, the gate and the parameters of an output that is not there, parameters of a norm that is not
+    if (!q->y.p && (q->post_kind != BIGMAC_NORM_NONE || q->gate.p || q->w_post || q->b_post)) return BIGMAC_ERR_INVALID_ARG;
+    if (!q->x.p) return BIGMAC_ERR_INVALID_ARG;
+    if (!backward) {
+        if (!rows_ok(q->r, q->d, es, &a->vec) || !rows_ok(q->n, q->d, es, &a->vec)) return BIGMAC_ERR_INVALID_ARG;
+        return (q->pre_kind == BIGMAC_NORM_NONE) == (q->n.p == nullptr) ? BIGMAC_OK : BIGMAC_ERR_INVALID_ARG;
+    }
+    ok = rows_ok(q->dr, q->d, es, &a->vec) && rows_ok(q->dn, q->d, es, &a->vec) && rows_ok(q->dx, q->d, es, &a->vec) && rows_ok(q->dy, q->d, es, &a->vec);
+    ok = ok && (q->gate_kind == BIGMAC_GATE_FULL ? rows_ok(q->dgate, q->d, es, &a->vec) : is_aligned(q->dgate.p, 4));
+    ok = ok && is_aligned(q->dw_post, 4) && is_aligned(q->db_post, 4) && is_aligned(q->dw_pre, 4) && is_aligned(q->db_pre, 4);
+    if (!ok || (!q->y.p && q->dy.p) || (q->pre_kind == BIGMAC_NORM_NONE && q->dn.p))
+        return BIGMAC_ERR_INVALID_ARG;
+    if (!q->stats || (!q->dr.p && !q->dn.p)) return BIGMAC_ERR_INVALID_ARG;
+    return BIGMAC_OK;
+}
+size_t residual_norm_scratch(const bigmac_residual_norm_t* q, int32_t T) {
+    const bool any = q->dw_post || q->db_post || q->dw_pre || q->db_pre || (q->gate_kind == BIGMAC_GATE_CHANNEL && q->dgate.p);
+    return any && T > 0 ? (size_t)residual_norm_parts(T, q->d) * 4 * q->d * sizeof(float) : 0;
+}
+
 }  // namespace
 
 extern "C" {
+
+int bigmac_residual_norm_forward(const bigmac_residual_norm_t* q, int32_t T, void* stream) {
+    ResNorm a;
+    const int s = check_residual_norm(q, T, false, &a);
+    if (s != BIGMAC_OK) return s;
+    return launch_residual_norm_forward(a, (cudaStream_t)stream) == cudaSuccess ? BIGMAC_OK : BIGMAC_ERR_CUDA;
+}
+
+int bigmac_residual_norm_scratch_bytes(const bigmac_residual_norm_t* q, int32_t T, size_t* scratch_bytes) {
+    if (!q || !scratch_bytes || T < 0 || q->d <= 0) return BIGMAC_ERR_INVALID_ARG;
+    if (q->d > kResNormMaxWidth) return BIGMAC_ERR_UNSUPPORTED;
+    *scratch_bytes = residual_norm_scratch(q, T);
+    return BIGMAC_OK;
+}
+
+int bigmac_residual_norm_backward(const bigmac_residual_norm_t* q, int32_t T, int accumulate, void* scratch, size_t scratch_bytes, void* stream) {
+    ResNorm a;
+    const int s = check_residual_norm(q, T, true, &a);
+    if (s != BIGMAC_OK) return s;
+    const size_t need = residual_norm_scratch(q, T);
+    if (need && (!scratch || !is_aligned(scratch, 16))) return BIGMAC_ERR_INVALID_ARG;
+    if (scratch_bytes < need) return BIGMAC_ERR_WORKSPACE;
+    return launch_residual_norm_backward(a, (float*)scratch, accumulate, (cudaStream_t)stream) == cudaSuccess ? BIGMAC_OK : BIGMAC_ERR_CUDA;
+}
 
 int bigmac_operator_status(void* stream) {
     int* at = status_word();

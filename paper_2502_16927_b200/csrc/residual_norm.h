@@ -1,0 +1,20 @@
+// The joint of two blocks (residual_norm.cu): r = rho x + gate * N_post(y), n = N_pre(r).
+#pragma once
+#include "internal.h"
+
+namespace bigmac {
+
+constexpr int kResNormMaxWidth = 8192;
+
+struct ResNorm {
+    const bigmac_residual_norm_t* q;
+    int T;
+    bool vec;                          // every row of every tensor on a 16-byte boundary, d a multiple of 8
+};
+
+cudaError_t launch_residual_norm_forward(const ResNorm& a, cudaStream_t stream);
+cudaError_t launch_residual_norm_backward(const ResNorm& a, float* partial, int accumulate, cudaStream_t stream);
+// Blocks of the backward pass: each leaves four vectors of d partial column sums.
+int residual_norm_parts(int T, int d);
+
+}  // namespace bigmac

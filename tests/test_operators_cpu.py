@@ -107,3 +107,55 @@ def test_reference_quantisation():
     v = ref.values(code, byte)[0]
     assert v[:10].tolist() == [6, -6, 6, 4, 4, 2, 2, 1, 0, 0.5]
     assert v[32:36].tolist() == [1.0, 0.0, -0.25, 0.25]
+
+
+# ---- the joint of two blocks
+
+_NAMES = ("d dtype post_kind pre_kind gate_kind post_eps pre_eps residual_scale w_post b_post w_pre b_pre x x_ld y y_ld gate gate_ld r r_ld n n_ld "
+          "stats dr dr_ld dn dn_ld dx dx_ld dy dy_ld dgate dgate_ld dw_post db_post dw_pre db_pre").split()
+
+
+def _joint(**kw):
+    base = dict.fromkeys(_NAMES, 0)
+    base.update(d=64, dtype=1, post_kind=1, pre_kind=2, post_eps=1e-6, pre_eps=1e-6, residual_scale=1.0, x=HERE, x_ld=64, y=HERE, y_ld=64, r=HERE, r_ld=64,
+                n=HERE, n_ld=64)
+    base.update(kw)
+    assert set(base) == set(_NAMES)
+    return binding._RESIDUAL_NORM.pack(*[base[n] for n in _NAMES])
+
+
+_BAD = [dict(d=0), dict(d=-1), dict(dtype=2), dict(post_kind=3), dict(pre_kind=-1), dict(gate_kind=4), dict(post_eps=-1e-6), dict(pre_eps=float("nan")),
+        dict(post_eps=float("inf")), dict(residual_scale=float("nan")), dict(x=HERE + 1), dict(x_ld=63), dict(y_ld=63), dict(x=0), dict(w_post=HERE + 2),
+        dict(gate_kind=1), dict(gate=HERE), dict(gate_kind=3, gate=HERE, gate_ld=63), dict(y=0), dict(y=0, post_kind=0, w_post=HERE),
+        dict(y=0, post_kind=0, gate_kind=1, gate=HERE), dict(stats=HERE + 4)]
+
+
+def test_residual_norm_refusals(lib):
+    assert lib.bigmac_residual_norm_forward(None, 1, None) == -1
+    for kw in _BAD + [dict(r=HERE + 1), dict(n_ld=63), dict(n=0), dict(pre_kind=0), dict(pre_kind=0, n=0, w_pre=HERE)]:
+        assert lib.bigmac_residual_norm_forward(_joint(**kw), 4, None) == -1, kw
+    assert lib.bigmac_residual_norm_forward(_joint(), -1, None) == -1
+    assert lib.bigmac_residual_norm_forward(_joint(d=8193, x_ld=8193, y_ld=8193), 4, None) == -2
+    assert lib.bigmac_residual_norm_forward(_joint(x=0, y=0, post_kind=0, r=0, n=0), 0, None) == 0       # no rows
+
+    back = dict(r=0, n=0, stats=HERE, dr=HERE, dr_ld=64, dn=HERE, dn_ld=64, dx=HERE, dx_ld=64, dy=HERE, dy_ld=64)
+
+    def call(scratch=HERE, size=1 << 30, T=4, **kw):
+        return lib.bigmac_residual_norm_backward(_joint(**{**back, **kw}), T, 0, scratch, size, None)
+
+    assert lib.bigmac_residual_norm_backward(None, 1, 0, None, 0, None) == -1
+    for kw in _BAD + [dict(stats=0), dict(dr=0, dn=0), dict(dx_ld=63), dict(dy=HERE + 1), dict(dgate=HERE), dict(pre_kind=0),
+                      dict(y=0, post_kind=0), dict(dw_post=HERE + 1), dict(dw_post=HERE, scratch=None), dict(dw_post=HERE, scratch=HERE + 8)]:
+        assert call(**kw) == -1, kw
+    assert call(dw_post=HERE, size=16) == -3
+
+    need = C.c_size_t()
+    assert lib.bigmac_residual_norm_scratch_bytes(_joint(**back), 4, C.byref(need)) == 0 and need.value == 0
+    assert lib.bigmac_residual_norm_scratch_bytes(_joint(**back, db_pre=HERE), 4, C.byref(need)) == 0 and need.value >= 4 * 64 * 4
+    assert lib.bigmac_residual_norm_scratch_bytes(_joint(**back, db_pre=HERE), 0, C.byref(need)) == 0 and need.value == 0
+    assert lib.bigmac_residual_norm_scratch_bytes(None, 4, C.byref(need)) == -1
+
+
+def test_binding_of_the_joint_refuses_tensors_of_the_cpu():
+    with pytest.raises(ValueError):
+        binding.residual_norm_forward(torch.zeros(4, 8), pre=binding.Norm(1))
