@@ -350,6 +350,47 @@ def operator_status() -> int:
     return lib().bigmac_operator_status(_stream())
 
 
+_DTYPES = {torch.float32: BIGMAC_F32, torch.bfloat16: BIGMAC_BF16}
+
+
+def _dtype(t: torch.dtype) -> int:
+    try:
+        return _DTYPES[t]
+    except KeyError:
+        raise ValueError(f"{t}: float32 and bfloat16 are supported") from None
+
+
+def _here() -> int:
+    """The current device: the kernels run on it, whatever device a tensor is on."""
+    return _current_device() if _current_device is not None else torch.cuda.current_device()
+
+
+def _dense(t: torch.Tensor, name: str, here: int) -> int:
+    if t.get_device() != here or not t.is_contiguous():
+        raise ValueError(f"{name}: a dense tensor on the current device, cuda:{here}, is needed")
+    return t.data_ptr()
+
+
+def _matrix(t: torch.Tensor, name: str, here: int):
+    """(address, row stride) of a matrix with dense rows."""
+    if t.get_device() == here and t.dim() == 2:
+        rows, columns = t.shape
+        if t.is_contiguous():
+            return t.data_ptr(), columns
+        ld, step = t.stride()
+        if (step == 1 or columns == 1) and (ld >= columns or rows == 1):
+            return t.data_ptr(), max(ld, columns)
+    raise ValueError(f"{name}: a matrix with dense rows that do not overlap, on the current device, cuda:{here}, is needed")
+
+
+def _vector(t: Optional[torch.Tensor], name: str, n: int, here: int) -> int:
+    if t is None:
+        return 0
+    if t.dtype is not torch.float32 or t.dim() != 1 or t.shape[0] != n:
+        raise ValueError(f"{name}: an fp32 vector of {n} is needed")
+    return _dense(t, name, here)
+
+
 BIGMAC_NORM_NONE, BIGMAC_NORM_RMS, BIGMAC_NORM_LAYER = 0, 1, 2
 BIGMAC_GATE_NONE, BIGMAC_GATE_TOKEN, BIGMAC_GATE_CHANNEL, BIGMAC_GATE_FULL = 0, 1, 2, 3
 
@@ -366,56 +407,44 @@ _NO_NORM = Norm(BIGMAC_NORM_NONE)
 # bigmac_residual_norm_t, packed at once: a ctypes structure of as many members takes longer to fill than a token's kernel runs
 _RESIDUAL_NORM = struct.Struct("@5i3f4P" + 5 * "Pq" + "P" + 5 * "Pq" + "4P")
 _NOTHING = (0, 0)
+_NO_BACKWARD = 14 * (0,)
 
 
-def _rows_like(t: Optional[torch.Tensor], name: str, shape, dtype):
-    """(address, row stride) of a [T, d] matrix of the joint, (0, 0) where there is none."""
+def _rows_like(t: Optional[torch.Tensor], name: str, x: torch.Tensor, here: int):
+    """(address, row stride) of a matrix of x's shape and type, (0, 0) where there is none."""
     if t is None:
         return _NOTHING
-    if t.dtype is not dtype or t.shape != shape:
-        raise ValueError(f"{name}: {tuple(shape)} of {dtype} is needed, not {tuple(t.shape)} of {t.dtype}")
-    return _rows_of(t, name)
-
-
-def _vector(t: Optional[torch.Tensor], name: str, n: int) -> int:
-    if t is None:
-        return 0
-    if t.dtype is not torch.float32 or t.dim() != 1 or t.shape[0] != n or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name}: a dense fp32 CUDA vector of {n} is needed")
-    return t.data_ptr()
+    if t.dtype is not x.dtype or t.shape != x.shape:
+        raise ValueError(f"{name}: {tuple(x.shape)} of {x.dtype} is needed, not {tuple(t.shape)} of {t.dtype}")
+    return _matrix(t, name, here)
 
 
 def _gate_kind(gate, x, gate_kind) -> int:
     """The gate's kind by its shape; a vector as long as both T and d is one factor a token unless gate_kind says otherwise."""
-    if gate is None:
-        kind = BIGMAC_GATE_NONE
-    elif gate.dim() == 2:
+    if gate.dim() == 2:
         kind = BIGMAC_GATE_FULL
-    elif gate_kind is not None:
-        kind = gate_kind
+    elif gate_kind in (BIGMAC_GATE_TOKEN, BIGMAC_GATE_CHANNEL):
+        return gate_kind
     else:
         kind = BIGMAC_GATE_TOKEN if gate.shape[0] == x.shape[0] else BIGMAC_GATE_CHANNEL
     if gate_kind is not None and kind != gate_kind:
-        raise ValueError(f"gate_kind {gate_kind}: the gate's shape says {kind}")
+        raise ValueError(f"gate_kind {gate_kind}: a gate of shape {tuple(gate.shape)}")
     return kind
 
 
-def _joint(x, y, gate, gate_kind, post, pre, residual_scale):
-    """The members of bigmac_residual_norm_t that forward and backward share, up to `gate`."""
-    if x.dim() != 2:
-        raise ValueError("x: [T, d]")
+def _joint(x, y, gate, gate_kind, post, pre, residual_scale, here):
+    """The members of bigmac_residual_norm_t that forward and backward share, up to `gate`, and the gate's kind."""
+    at = _matrix(x, "x", here)
     T, d = x.shape
-    at = _rows_of(x, "x")
-    kind = _gate_kind(gate, x, gate_kind)
-    post, pre = post or _NO_NORM, pre or _NO_NORM
-    if kind == BIGMAC_GATE_FULL:
-        g = _rows_like(gate, "gate", x.shape, x.dtype)
-    else:
-        g = (_vector(gate, "gate", T if kind == BIGMAC_GATE_TOKEN else d), 0)
-    _same_device(x, y, gate, post.weight, post.bias, pre.weight, pre.bias)
-    return (d, _dtype(x.dtype), post.kind, pre.kind, kind, post.eps, pre.eps, residual_scale, _vector(post.weight, "post.weight", d),
-            _vector(post.bias, "post.bias", d), _vector(pre.weight, "pre.weight", d), _vector(pre.bias, "pre.bias", d), *at,
-            *_rows_like(y, "y", x.shape, x.dtype), *g), kind
+    kind, g = BIGMAC_GATE_NONE, _NOTHING
+    if gate is not None:
+        kind = _gate_kind(gate, x, gate_kind)
+        g = _rows_like(gate, "gate", x, here) if kind == BIGMAC_GATE_FULL else (_vector(gate, "gate", T if kind == BIGMAC_GATE_TOKEN else d, here), 0)
+    post_kind, w_post, b_post, post_eps = post or _NO_NORM
+    pre_kind, w_pre, b_pre, pre_eps = pre or _NO_NORM
+    return (d, _dtype(x.dtype), post_kind, pre_kind, kind, post_eps, pre_eps, residual_scale, _vector(w_post, "post.weight", d, here),
+            _vector(b_post, "post.bias", d, here), _vector(w_pre, "pre.weight", d, here), _vector(b_pre, "pre.bias", d, here), *at,
+            *_rows_like(y, "y", x, here), *g), kind
 
 
 def residual_norm_forward(x: torch.Tensor, y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, post: Optional[Norm] = None,
@@ -423,16 +452,16 @@ def residual_norm_forward(x: torch.Tensor, y: Optional[torch.Tensor] = None, gat
                           r: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None):
     """r = residual_scale x + gate N_post(y) and n = N_pre(r) (bigmac_residual_norm_forward): (r, n, stats), n None without `pre`, stats (for
     the backward) None unless `training`.  gate: [T] or [d] fp32, or [T, d].  r and n may be given, in place too (r is x, n is y)."""
-    members, _ = _joint(x, y, gate, gate_kind, post, pre, residual_scale)
+    here = _here()
+    members, _ = _joint(x, y, gate, gate_kind, post, pre, residual_scale, here)
+    T, d = x.shape
     if r is None:
-        r = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    if n is None and pre is not None and pre.kind != BIGMAC_NORM_NONE:
-        n = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    stats = torch.empty((x.shape[0], 4), dtype=torch.float32, device=x.device) if training else None
-    _same_device(r, n)
-    q = _RESIDUAL_NORM.pack(*members, *_rows_like(r, "r", x.shape, x.dtype), *_rows_like(n, "n", x.shape, x.dtype),
-                            0 if stats is None else stats.data_ptr(), *(14 * (0,)))
-    _check(lib().bigmac_residual_norm_forward(q, x.shape[0], _stream()), "bigmac_residual_norm_forward")
+        r = torch.empty_like(x)
+    if n is None and members[3] != BIGMAC_NORM_NONE:
+        n = torch.empty_like(x)
+    stats = torch.empty((T, 4), dtype=torch.float32, device=x.device) if training else None
+    q = _RESIDUAL_NORM.pack(*members, *_rows_like(r, "r", x, here), *_rows_like(n, "n", x, here), 0 if stats is None else stats.data_ptr(), *_NO_BACKWARD)
+    _check(lib().bigmac_residual_norm_forward(q, T, _stream()), "bigmac_residual_norm_forward")
     return r, n, stats
 
 
@@ -441,24 +470,25 @@ def residual_norm_backward(x, y, gate, post, pre, dr, dn, stats, G: Optional[Dic
     """Gradients of sum(r dr) + sum(n dn) (bigmac_residual_norm_backward): (dx, dy, dgate), None for what was not in the call.  G holds
     fp32 buffers for the gradients of the parameters, any of dw_post, db_post, dw_pre, db_pre and, for a gate [d], dgate (returned,
     too); with `accumulate` they are added to.  dr or dn may be None."""
-    members, kind = _joint(x, y, gate, gate_kind, post, pre, residual_scale)
+    here = _here()
+    members, kind = _joint(x, y, gate, gate_kind, post, pre, residual_scale, here)
     G, (T, d) = G or {}, x.shape
-    dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    dy = None if y is None else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    dx = torch.empty_like(x)
+    dy = None if y is None else torch.empty_like(x)
     if kind == BIGMAC_GATE_CHANNEL:
         dgate = G.get("dgate")
-        dg = (_vector(dgate, "dgate", d), 0)
+        dg = (_vector(dgate, "dgate", d, here), 0)
     elif kind == BIGMAC_GATE_NONE:
         dgate, dg = None, _NOTHING
     else:
-        dgate = torch.empty(gate.shape, dtype=gate.dtype, device=x.device)
+        dgate = torch.empty_like(gate)
         dg = (dgate.data_ptr(), d)
-    if stats is None or stats.dtype is not torch.float32 or stats.shape != (T, 4) or not stats.is_contiguous():
+    if stats is None or stats.dtype is not torch.float32 or stats.shape != (T, 4):
         raise ValueError("stats: those of a training forward of the same rows")
-    grads = [_vector(G.get(name), name, d) for name in ("dw_post", "db_post", "dw_pre", "db_pre")]
-    _same_device(dr, dn, stats, *G.values())
-    q = _RESIDUAL_NORM.pack(*members, 0, 0, 0, 0, stats.data_ptr(), *_rows_like(dr, "dr", x.shape, x.dtype), *_rows_like(dn, "dn", x.shape, x.dtype),
-                            dx.data_ptr(), d, *((0, 0) if dy is None else (dy.data_ptr(), d)), *dg, *grads)
+    q = _RESIDUAL_NORM.pack(*members, 0, 0, 0, 0, _dense(stats, "stats", here), *_rows_like(dr, "dr", x, here), *_rows_like(dn, "dn", x, here),
+                            dx.data_ptr(), d, *(_NOTHING if dy is None else (dy.data_ptr(), d)), *dg, _vector(G.get("dw_post"), "dw_post", d, here),
+                            _vector(G.get("db_post"), "db_post", d, here), _vector(G.get("dw_pre"), "dw_pre", d, here),
+                            _vector(G.get("db_pre"), "db_pre", d, here))
     need = C.c_size_t()
     _check(lib().bigmac_residual_norm_scratch_bytes(q, T, C.byref(need)), "bigmac_residual_norm_scratch_bytes")
     scratch = torch.empty(need.value, dtype=torch.uint8, device=x.device) if need.value else None
@@ -477,22 +507,24 @@ class Mx4(NamedTuple):
     rows: Optional[int] = None
 
 
-def _mx4(q: Mx4) -> bigmac_mx4_t:
-    codes, scales, offsets = q.codes, q.scales, q.offsets
-    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or codes.dim() not in (2, 3) or scales.dim() != codes.dim() + 1:
-        raise ValueError("Mx4: codes [rows, K / 2] and scales [row tiles, K tiles, 512] of torch.uint8, or both with a leading E")
-    *lead, stored, half = codes.shape
-    if tuple(scales.shape) != (*lead, -(-stored // 128), -(-half // 64), 512):
-        raise ValueError(f"Mx4: codes of shape {tuple(codes.shape)} have scales of shape {(*lead, -(-stored // 128), -(-half // 64), 512)}")
-    rows, E = stored, lead[0] if lead else 0
-    if offsets is not None:
-        if lead or offsets.dtype != torch.int32 or offsets.dim() != 1 or offsets.numel() < 2 or q.rows is None:
-            raise ValueError("a grouped Mx4 has codes of two dimensions, int32 offsets [E + 1] and rows")
-        rows, E = q.rows, offsets.numel() - 1
+def _mx4(q: Mx4, here: int) -> bigmac_mx4_t:
+    codes, scales, offsets, rows = q
+    shape = codes.shape
+    stored, half, E = shape[-2] if len(shape) > 1 else 0, shape[-1], shape[0] if len(shape) == 3 else 0
+    tiles = (-(-stored // 128), -(-half // 64), 512)
+    if (codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or not 1 < len(shape) < 4 or
+            scales.shape != (tiles if len(shape) == 2 else (E, *tiles))):
+        raise ValueError(f"Mx4: codes [rows, K / 2] and scales [row tiles, K tiles, 512] of torch.uint8, or both with a leading E; not "
+                         f"{tuple(shape)} and {tuple(scales.shape)}")
+    if offsets is None:
+        rows = stored
+    else:
+        if E or rows is None:
+            raise ValueError("a grouped Mx4 has codes of two dimensions and rows")
+        E = _offsets(offsets, here)
         if stored < _mx4_stored(rows, E):
             raise ValueError(f"Mx4: {rows} rows of {E} experts need {_mx4_stored(rows, E)} rows of codes")
-    _same_device(codes, scales, offsets)
-    return bigmac_mx4_t(_ptr(codes), _ptr(scales), rows, 2 * half, E, _ptr(offsets))
+    return bigmac_mx4_t(_dense(codes, "codes", here), _dense(scales, "scales", here), rows, 2 * half, E, None if offsets is None else offsets.data_ptr())
 
 
 def _mx4_stored(rows: int, E: int) -> int:
@@ -500,75 +532,64 @@ def _mx4_stored(rows: int, E: int) -> int:
     return (rows + min(rows, E) * 127) // 128 * 128
 
 
-def _same_device(*tensors) -> None:
-    """The kernels run on the current device: a tensor of another one would be read through its address there."""
-    here = _current_device() if _current_device is not None else torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != here:
-            raise ValueError(f"tensor on {t.device}, the current device is cuda:{here}")
-
-
-_DTYPES = {torch.float32: BIGMAC_F32, torch.bfloat16: BIGMAC_BF16}
-
-
-def _dtype(t: torch.dtype) -> int:
-    try:
-        return _DTYPES[t]
-    except KeyError:
-        raise ValueError(f"{t}: float32 and bfloat16 are supported") from None
-
-
-def _rows_of(t: torch.Tensor, name: str):
-    """(address, row stride) of a matrix whose rows are dense."""
-    if not t.is_cuda or t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-        raise ValueError(f"{name}: a CUDA matrix with dense rows that do not overlap is needed")
-    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1]
+def _offsets(t: torch.Tensor, here: int) -> int:
+    """The number of experts of a table of segments."""
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] < 2:
+        raise ValueError("offsets: an int32 vector [E + 1] is needed")
+    _dense(t, "offsets", here)
+    return t.shape[0] - 1
 
 
 def mx4_quantize(x: torch.Tensor, offsets: Optional[torch.Tensor] = None, slot_of_row: Optional[torch.Tensor] = None, k: int = 1) -> Mx4:
     """Rows of x to 4 bits (bigmac_mx4_quantize).  With `offsets` (int32 [E + 1], of a routing) grouped by expert; with `slot_of_row`
     row i is x[slot_of_row[i] // k]: the dispatch."""
-    ptr, ld = _rows_of(x, "x")
-    for name, t in (("offsets", offsets), ("slot_of_row", slot_of_row)):
-        if t is not None and (t.dtype != torch.int32 or t.dim() != 1 or not t.is_cuda or not t.is_contiguous()):
-            raise ValueError(f"{name}: a dense int32 CUDA vector is needed")
-    _same_device(x, offsets, slot_of_row)
-    rows, K = x.shape[0] if slot_of_row is None else slot_of_row.numel(), x.shape[1]
+    here = _here()
+    ptr, ld = _matrix(x, "x", here)
+    x_rows, K = x.shape
+    rows, slots, E, table = x_rows, None, 0, None
     if K == 0 or K % 32:
         raise ValueError(f"K = {K}: blocks of 32 columns")
-    E = 0 if offsets is None else offsets.numel() - 1
-    stored = rows if offsets is None else _mx4_stored(rows, E)
-    codes = torch.empty((stored, K // 2), dtype=torch.uint8, device=x.device)
-    scales = torch.empty((-(-stored // 128), -(-K // 128), 512), dtype=torch.uint8, device=x.device)
-    q = bigmac_mx4_t(codes.data_ptr(), scales.data_ptr(), rows, K, E, None if offsets is None else offsets.data_ptr())
-    _check(lib().bigmac_mx4_quantize(ptr, _dtype(x.dtype), x.shape[0], ld, None if slot_of_row is None else slot_of_row.data_ptr(), k, C.byref(q),
-                                     _stream()), "bigmac_mx4_quantize")
+    if slot_of_row is not None:
+        if slot_of_row.dtype is not torch.int32 or slot_of_row.dim() != 1:
+            raise ValueError("slot_of_row: an int32 vector is needed")
+        slots, rows = _dense(slot_of_row, "slot_of_row", here), slot_of_row.shape[0]
+    stored = rows
+    if offsets is not None:
+        E, table = _offsets(offsets, here), offsets.data_ptr()
+        stored = _mx4_stored(rows, E)
+    device = x.device
+    codes = torch.empty((stored, K // 2), dtype=torch.uint8, device=device)
+    scales = torch.empty((-(-stored // 128), -(-K // 128), 512), dtype=torch.uint8, device=device)
+    q = bigmac_mx4_t(codes.data_ptr(), scales.data_ptr(), rows, K, E, table)
+    _check(lib().bigmac_mx4_quantize(ptr, _dtype(x.dtype), x_rows, ld, slots, k, C.byref(q), _stream()), "bigmac_mx4_quantize")
     return Mx4(codes, scales, offsets, rows)
+
+
+def _output(out, rows: int, columns: int, dtype, device, here: int):
+    """The result's matrix: (tensor, address, row stride, bigmac_dtype_t)."""
+    if out is None:
+        out = torch.empty((rows, columns), dtype=dtype, device=device)
+        return out, out.data_ptr(), columns, _dtype(dtype)
+    if out.shape != (rows, columns):
+        raise ValueError(f"out has shape {tuple(out.shape)}, not {(rows, columns)}")
+    return (out, *_matrix(out, "out", here), _dtype(out.dtype))
 
 
 def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The numbers a matrix stands for, in the caller's order of rows.  Of a grouped one, rows in no segment keep what `out` holds."""
-    c = _mx4(q)
-    if out is None:
-        out = torch.empty((c.rows, c.K), dtype=dtype, device=q.codes.device)
-    elif tuple(out.shape) != (c.rows, c.K):
-        raise ValueError(f"out has shape {tuple(out.shape)}, not {(c.rows, c.K)}")
-    ptr, ld = _rows_of(out, "out")
-    _same_device(out)
-    _check(lib().bigmac_mx4_dequantize(C.byref(c), ptr, _dtype(out.dtype), ld, _stream()), "bigmac_mx4_dequantize")
+    here = _here()
+    c = _mx4(q, here)
+    out, ptr, ld, kind = _output(out, c.rows, c.K, dtype, q.codes.device, here)
+    _check(lib().bigmac_mx4_dequantize(C.byref(c), ptr, kind, ld, _stream()), "bigmac_mx4_dequantize")
     return out
 
 
 def mx4_matmul(a: Mx4, w: Mx4, act: int = 3, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """act(a w^T) (bigmac_mx4_matmul; act a bigmac_act_t, 3 the identity).  For a grouped `a`, `w` holds the matrices of its experts."""
-    ca, cw = _mx4(a), _mx4(w)
-    if out is None:
-        out = torch.empty((ca.rows, cw.rows), dtype=dtype, device=a.codes.device)
-    elif tuple(out.shape) != (ca.rows, cw.rows):
-        raise ValueError(f"out has shape {tuple(out.shape)}, not {(ca.rows, cw.rows)}")
-    ptr, ld = _rows_of(out, "out")
-    _same_device(out)
-    _check(lib().bigmac_mx4_matmul(C.byref(ca), C.byref(cw), act, _dtype(out.dtype), ptr, ld, _stream()), "bigmac_mx4_matmul")
+    here = _here()
+    ca, cw = _mx4(a, here), _mx4(w, here)
+    out, ptr, ld, kind = _output(out, ca.rows, cw.rows, dtype, a.codes.device, here)
+    _check(lib().bigmac_mx4_matmul(C.byref(ca), C.byref(cw), act, kind, ptr, ld, _stream()), "bigmac_mx4_matmul")
     return out
 
 

@@ -61,6 +61,28 @@ __host__ __device__ constexpr uint32_t instr_desc_mx4(int bn, int half) {
            ((uint32_t)(2 * half) << 29);
 }
 
+// GELU of 32 accumulators for an output in bf16:  gelu(z) = max(z, 0) - u Q(u),  u = |z|,  Q(u) = Phi(-u) = exp(-u^2/2) G(u).  G(u) = erfcx(u / sqrt 2) / 2
+// falls smoothly from 1/2 to 0.08; the polynomial of degree 9 in u - 2.5 below is its minimax fit in relative error on [0, 5] (fitted
+// by reweighted least squares on Chebyshev nodes), 3.2e-5 in fp32, so the negative tail keeps its relative precision, too.  Behind 5 the arguments of u and
+// G stay at 5 (the term is below 2e-6 there; an infinity gives infinity or 0).  One special function and eight packed
+// instructions an element; erff takes three times the instructions, and with it the call for 131072 rows of r 256, h 1024 took 200 us.
+__device__ __forceinline__ void gelu_chunk(float* v) {
+    constexpr float kGeluC[10] = {0.14133550226688385f, -0.045609001070261f, 0.013612025417387486f, -0.0038369703106582165f, 0.0010656173108145595f,
+                                  -0.0002591590746305883f, 4.105969856027514e-05f, -1.1991459359705914e-05f, 6.8091194407315925e-06f, -1.2926340104968403e-06f};
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const float z0 = v[2 * i], z1 = v[2 * i + 1];
+        const f32x2_t z = pk2(z0, z1), u = pk2(fminf(fabsf(z0), 5.0f), fminf(fabsf(z1), 5.0f)), s = add2(u, pk2(-2.5f, -2.5f));
+        f32x2_t P = pk2(kGeluC[9], kGeluC[9]);
+#pragma unroll
+        for (int k = 8; k >= 0; --k) P = fma2(P, s, pk2(kGeluC[k], kGeluC[k]));
+        float e0, e1;
+        upk2(mul2(mul2(z, z), pk2(-0.72134752f, -0.72134752f)), e0, e1);
+        const f32x2_t Q = mul2(P, pk2(fast_ex2(e0), fast_ex2(e1)));
+        upk2(fma2(mul2(u, pk2(-1.0f, -1.0f)), Q, pk2(fmaxf(z0, 0.0f), fmaxf(z1, 0.0f))), v[2 * i], v[2 * i + 1]);
+    }
+}
+
 struct Mx4Tile {
     int a_row;                                             // first row in A's storage
     int n0, expert;
@@ -241,7 +263,9 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 }
                 const int col0 = q.n0 + chunk * 32;
                 if (!have || col0 >= p.N || !row_ok) continue;
-                if (p.act != BIGMAC_ACT_IDENTITY) {
+                if (p.act == BIGMAC_ACT_GELU_ERF && !p.out_f32) {
+                    gelu_chunk(v);
+                } else if (p.act != BIGMAC_ACT_IDENTITY) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = act_apply(p.act, v[i]);
                 }

@@ -90,9 +90,7 @@ def test_binding_refuses_what_is_no_4_bit_matrix():
                               (torch.zeros(4, 32, dtype=u8), torch.zeros(1, 1, 512, dtype=u8), dict(offsets=torch.zeros(3, dtype=torch.int32))),
                               (torch.zeros(4, 32, dtype=u8), torch.zeros(1, 1, 512, dtype=u8), dict(offsets=torch.zeros(3, dtype=torch.int32), rows=4))):
         with pytest.raises(ValueError):
-            binding._mx4(binding.Mx4(codes, scales, **kw))
-    with pytest.raises(ValueError):
-        binding.mx4_quantize(torch.zeros(4, 64))                        # not on a GPU
+            binding._mx4(binding.Mx4(codes, scales, **kw), -1)
     with pytest.raises(ValueError):
         binding._dtype(torch.float16)
 
@@ -154,8 +152,3 @@ def test_residual_norm_refusals(lib):
     assert lib.bigmac_residual_norm_scratch_bytes(_joint(**back, db_pre=HERE), 4, C.byref(need)) == 0 and need.value >= 4 * 64 * 4
     assert lib.bigmac_residual_norm_scratch_bytes(_joint(**back, db_pre=HERE), 0, C.byref(need)) == 0 and need.value == 0
     assert lib.bigmac_residual_norm_scratch_bytes(None, 4, C.byref(need)) == -1
-
-
-def test_binding_of_the_joint_refuses_tensors_of_the_cpu():
-    with pytest.raises(ValueError):
-        binding.residual_norm_forward(torch.zeros(4, 8), pre=binding.Norm(1))
