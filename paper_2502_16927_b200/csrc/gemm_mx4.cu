@@ -8,7 +8,10 @@
 // Persistent CTAs walk the 128 x BN tiles of C.  Warp 0 streams slices of 256 columns into a ring of stages: codes by TMA (128 bytes a
 // row, 128-byte swizzle), scale bytes by bulk copies (512 bytes for 128 rows and 128 columns).  Warp 1 moves a slice's scale
 // bytes to tensor memory (tcgen05.cp, in order before the products that read them, as the products before it are in order before the
-// copy: one buffer is enough) and issues the products.  The other warps drain a finished accumulator while the next one fills.
+// copy: one buffer is enough) and issues the products.  Two sets of eight warps drain the two accumulators in turn, each while the other's
+// fills and the other set stores: with all sixteen on one accumulator every latency of a tile (barrier, tensor memory, stores) was waited out
+// by all (131072 rows, r 256 -> h 1024: 142 us).  bf16 rows leave through shared memory and TMA, 128 bytes a row; 32-byte stores of the
+// lanes' own rows alone took 1350 cycles a tile.
 #include "tc_common.cuh"
 #include "mx4.h"
 
@@ -21,7 +24,7 @@ namespace {
 constexpr int kSliceK = 256;                               // columns of a stage: one 128-byte row of codes
 constexpr uint32_t kABytes = 128 * 128;
 constexpr uint32_t kSfTile = 512;
-constexpr int kEpi = 16;                                   // epilogue warps, four to a lane quadrant
+constexpr int kEpi = 16;                                   // epilogue warps, two sets with two to a lane quadrant
 constexpr int kThreadsMx4 = (2 + kEpi) * 32;
 
 struct Mx4Params {
@@ -31,7 +34,7 @@ struct Mx4Params {
     const int32_t* offsets;                                // grouped: the caller's table
     int M, N, K, E;
     int64_t capacity;                                      // rows that A has room for (grouped)
-    int act, out_f32;
+    int act, out_f32, tma_store;
     int* status;
 };
 
@@ -83,30 +86,47 @@ __device__ __forceinline__ void gelu_chunk(float* v) {
     }
 }
 
-struct Mx4Tile {
-    int a_row;                                             // first row in A's storage
-    int n0, expert;
-    int c_row, rows;                                       // first row in C, rows of this tile that exist
+// The tiles of a walker: t, t + step, ...  All columns of a row tile follow each other (its codes stay in L2).
+struct Mx4Tables {                                         // grouped: shared memory
+    const int32_t *prefix, *first, *end;                   // row tiles before expert e [E + 1]; its rows in the caller's order
 };
-
-// Tile t: all columns of a row tile after each other (its codes stay in L2).
-__device__ __forceinline__ Mx4Tile mx4_tile(const Mx4Params& p, const int32_t* prefix, int BN, int t, int tiles_n) {
-    Mx4Tile q;
-    const int mt = t / tiles_n;
-    q.n0 = (t - mt * tiles_n) * BN;
-    q.a_row = mt * kMx4Tile;
-    if (p.offsets) {
-        q.expert = mx4_find(prefix, p.E, mt);
-        const Mx4Segment s = mx4_segment(p.offsets, q.expert, p.M);
-        const int at = (mt - prefix[q.expert]) * kMx4Tile;
-        q.c_row = s.first + at;
-        q.rows = min(kMx4Tile, s.count - at);
-    } else {
-        q.expert = 0;
-        q.c_row = q.a_row;
-        q.rows = min(kMx4Tile, p.M - q.a_row);
+struct Mx4Walk {
+    int mt, nt, e, step_m, step_n, tiles_n;
+    __device__ __forceinline__ void init(int t, int step, int n) {
+        tiles_n = n;
+        mt = t / n; nt = t - mt * n;
+        step_m = step / n; step_n = step - step_m * n;
+        e = 0;
     }
-    return q;
+    __device__ __forceinline__ void next() {
+        mt += step_m; nt += step_n;
+        if (nt >= tiles_n) { nt -= tiles_n; ++mt; }
+    }
+    // The expert of row tile mt, which never falls from tile to tile.
+    __device__ __forceinline__ int expert(const Mx4Tables& tb, int E) {
+        while (e + 1 < E && tb.prefix[e + 1] <= mt) ++e;
+        return e;
+    }
+};
+struct Mx4Rows {
+    int expert, c_row, rows;                               // first row in C, rows of this tile that exist
+};
+__device__ __forceinline__ Mx4Rows mx4_rows(const Mx4Params& p, const Mx4Tables& tb, Mx4Walk& w) {
+    if (!p.offsets) return {0, w.mt * kMx4Tile, min(kMx4Tile, p.M - w.mt * kMx4Tile)};
+    const int e = w.expert(tb, p.E), c = tb.first[e] + (w.mt - tb.prefix[e]) * kMx4Tile;
+    return {e, c, min(kMx4Tile, tb.end[e] - c)};
+}
+
+// 32 columns of a row, packed, to the warp's box of 32 rows by COLS columns, laid out for a TMA store with the swizzle of its row's width.
+template <int COLS>
+__device__ __forceinline__ void stage_row(uint8_t* box, int lane, int chunk, const uint32_t* w) {
+    if (COLS == 64) {
+        uint8_t* row = box + lane * 128;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) st_shared_16B(row + (((chunk * 4 + j) ^ (lane & 7)) << 4), w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    } else {
+        stage_row_bf16(box, lane, w);
+    }
 }
 
 template <int BN, int STAGES>
@@ -116,37 +136,41 @@ struct Mx4Smem {
     static constexpr uint32_t kSfBytes = 2 * kSfTile * (1 + kWTiles);    // A's two k tiles, then W's
     static constexpr uint32_t kStage = kABytes + kBBytes + kSfBytes;     // a multiple of 1024
     static_assert(kStage % 1024 == 0, "128-byte swizzle: stages on 1024-byte boundaries");
+    static constexpr int kCols = BN / 2;                                 // columns of an epilogue warp
+    static constexpr uint32_t kBox = 32 * kCols * 2;
     static constexpr uint32_t kBars = (2 * STAGES + 4) * 8 + 16;
-    static size_t bytes(int E) { return 1024 + STAGES * kStage + kBars + (size_t)(E + 1) * 4; }
+    static constexpr size_t bytes(int E) { return 1024 + STAGES * kStage + kEpi * kBox + kBars + (size_t)(3 * E + 1) * 4; }
 };
 
 template <int BN, int STAGES>
 __global__ void __launch_bounds__(kThreadsMx4, 1)
 gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32, const __grid_constant__ CUtensorMap map_w,
-                const Mx4Params p) {
+                const __grid_constant__ CUtensorMap map_c, const Mx4Params p) {
     using S = Mx4Smem<BN, STAGES>;
-    constexpr uint32_t kAcc = BN > 128 ? 1 : 2;                          // accumulators
-    constexpr uint32_t kSfCol = kAcc * BN;                               // scale bytes behind them: A's 8 columns, then W's
+    constexpr uint32_t kSfCol = 2 * BN;                                  // scale bytes behind them: A's 8 columns, then W's
     constexpr uint32_t kTmemCols = kSfCol + 8 + 8 * S::kWTiles <= 256 ? 256 : 512;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    uint64_t* full_bar = (uint64_t*)(smem + STAGES * S::kStage);
+    uint8_t* boxes_c = smem + STAGES * S::kStage;
+    uint64_t* full_bar = (uint64_t*)(boxes_c + kEpi * S::kBox);
     uint64_t* empty_bar = full_bar + STAGES;
     uint64_t* tmem_full_bar = empty_bar + STAGES;                        // [2]
     uint64_t* tmem_empty_bar = tmem_full_bar + 2;                        // [2]
     uint32_t* tmem_slot = (uint32_t*)(tmem_empty_bar + 2);
     volatile int* dead = (volatile int*)(tmem_slot + 1);
-    int32_t* prefix = (int32_t*)(tmem_slot + 4);                         // [E + 1]
+    int32_t* tables = (int32_t*)(tmem_slot + 4);
+    const Mx4Tables tb{tables, tables + p.E + 1, tables + 2 * p.E + 1};
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 32) {
         prefetch_tensormap(&map_a);
         prefetch_tensormap(&map_a32);
         prefetch_tensormap(&map_w);
+        prefetch_tensormap(&map_c);
     }
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(&full_bar[s], 1); mbar_init(&empty_bar[s], 1); }
-        for (int s = 0; s < 2; ++s) { mbar_init(&tmem_full_bar[s], 1); mbar_init(&tmem_empty_bar[s], kEpi); }
+        for (int s = 0; s < 2; ++s) { mbar_init(&tmem_full_bar[s], 1); mbar_init(&tmem_empty_bar[s], kEpi / 2); }
         *dead = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -157,14 +181,19 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     grid_dependency_launch();
     grid_dependency_wait();
     if (p.offsets) {
-        if (warp == 2) mx4_tile_prefix(p.offsets, p.E, p.M, prefix);
+        if (warp == 2) mx4_tile_prefix(p.offsets, p.E, p.M, tables);
+        for (int e = (int)threadIdx.x - 96; e >= 0 && e < p.E; e += kThreadsMx4 - 96) {
+            const Mx4Segment seg = mx4_segment(p.offsets, e, p.M);
+            tables[p.E + 1 + e] = seg.first;
+            tables[2 * p.E + 1 + e] = seg.first + seg.count;
+        }
         __syncthreads();
     }
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     const int ktiles = mx4_ktiles(p.K), num_kb = (p.K + kSliceK - 1) / kSliceK;
     const int tiles_n = (p.N + BN - 1) / BN;
-    const int tiles_m = p.offsets ? (int)min((int64_t)prefix[p.E], p.capacity / kMx4Tile) : (p.M + kMx4Tile - 1) / kMx4Tile;
+    const int tiles_m = p.offsets ? (int)min((int64_t)tb.prefix[p.E], p.capacity / kMx4Tile) : (p.M + kMx4Tile - 1) / kMx4Tile;
     const int total = tiles_m * tiles_n;
 
     if (warp == 0) {
@@ -172,10 +201,12 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         if (elect_one()) {
             const int w_row_tiles = (p.N + 127) / 128;
             uint32_t s = 0, phase = 1;
-            for (int t = blockIdx.x; t < total; t += gridDim.x) {
-                const Mx4Tile q = mx4_tile(p, prefix, BN, t, tiles_n);
-                const uint8_t* sa = p.sa + (int64_t)(q.a_row / 128) * ktiles * kSfTile;
-                const int wt = q.n0 / 128;
+            Mx4Walk walk;
+            walk.init(blockIdx.x, gridDim.x, tiles_n);
+            for (int t = blockIdx.x; t < total; t += gridDim.x, walk.next()) {
+                const Mx4Rows q = mx4_rows(p, tb, walk);
+                const int a_row = walk.mt * kMx4Tile, n0 = walk.nt * BN, wt = n0 / 128;
+                const uint8_t* sa = p.sa + (int64_t)walk.mt * ktiles * kSfTile;
                 const uint8_t* sw = p.sw + ((int64_t)q.expert * w_row_tiles + wt) * ktiles * kSfTile;
                 const int w_tiles = min(S::kWTiles, w_row_tiles - wt);
                 const int boxes = q.rows > 96 ? 0 : (q.rows + 31) / 32;  // of 32 rows; 0: all 128 in one
@@ -187,9 +218,9 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     uint8_t* a = smem + s * S::kStage;
                     uint8_t* b = a + kABytes;
                     uint8_t* f = b + S::kBBytes;
-                    if (boxes) for (int i = 0; i < boxes; ++i) tma_load_2d(a + i * 32 * 128, &map_a32, &full_bar[s], kb * 128, q.a_row + 32 * i);
-                    else tma_load_2d(a, &map_a, &full_bar[s], kb * 128, q.a_row);
-                    tma_load_2d(b, &map_w, &full_bar[s], kb * 128, q.expert * p.N + q.n0);
+                    if (boxes) for (int i = 0; i < boxes; ++i) tma_load_2d(a + i * 32 * 128, &map_a32, &full_bar[s], kb * 128, a_row + 32 * i);
+                    else tma_load_2d(a, &map_a, &full_bar[s], kb * 128, a_row);
+                    tma_load_2d(b, &map_w, &full_bar[s], kb * 128, q.expert * p.N + n0);
                     bulk_load(f, sa + kb * 2 * kSfTile, sf, &full_bar[s]);
                     for (int i = 0; i < w_tiles; ++i)
                         bulk_load(f + 2 * kSfTile * (1 + i), sw + ((int64_t)i * ktiles + kb * 2) * kSfTile, sf, &full_bar[s]);
@@ -203,7 +234,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             const uint64_t df0 = scale_desc(smem_u32(smem + kABytes + S::kBBytes));
             uint32_t stage = 0, phase = 0, local = 0;
             for (int t = blockIdx.x; t < total; t += gridDim.x, ++local) {
-                const uint32_t acc = kAcc == 2 ? local & 1 : 0, use = kAcc == 2 ? local >> 1 : local;
+                const uint32_t acc = local & 1, use = local >> 1;
                 // a 64-column tile in the second half of W's row tile: its rows' bytes start two columns further
                 const uint32_t shift = BN == 64 ? (uint32_t)((t % tiles_n) & 1) * 2 : 0;
                 mbar_wait_lean(&tmem_empty_bar[acc], (use & 1) ^ 1, dead, p.status);
@@ -236,33 +267,41 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             }
         }
     } else {
-        // ------------------------------------------------------------------ epilogue
-        const int quad = warp & 3, part = (warp - 2) >> 2;
-        constexpr int kChunks = BN / 32, kPerWarp = (kChunks + 3) / 4;   // chunks of 32 columns: part, part + 4, ...
-        uint32_t local = 0;
+        // ------------------------------------------------------------------ epilogue: set `acc` drains accumulator `acc`
+        const int quad = warp & 3, half = ((warp - 2) >> 2) & 1;
+        const uint32_t acc = (uint32_t)(warp - 2) >> 3;
+        constexpr int kChunks = S::kCols / 32;
+        uint8_t* box = boxes_c + (warp - 2) * S::kBox;
         const int esz = p.out_f32 ? 4 : 2;
         const bool vec_ok = (p.ldc * esz) % 32 == 0 && (uintptr_t)p.C % 32 == 0;
-        for (int t = blockIdx.x; t < total; t += gridDim.x, ++local) {
-            const Mx4Tile q = mx4_tile(p, prefix, BN, t, tiles_n);
-            const uint32_t acc = kAcc == 2 ? local & 1 : 0, use = kAcc == 2 ? local >> 1 : local;
+        const uint32_t t_addr = tmem + acc * BN + ((uint32_t)(quad * 32) << 16) + half * S::kCols;
+        uint32_t use = 0;
+        Mx4Walk walk;
+        walk.init(blockIdx.x + acc * gridDim.x, 2 * gridDim.x, tiles_n);
+        for (int t = blockIdx.x + acc * gridDim.x; t < total; t += 2 * gridDim.x, walk.next(), ++use) {
+            const Mx4Rows q = mx4_rows(p, tb, walk);
+            const int first_col = walk.nt * BN + half * S::kCols, row = quad * 32 + lane;
+            const bool row_ok = row < q.rows;
+            // whole boxes by TMA (a dense C is cut off by the tensor map); the last rows of a segment row by row
+            const bool by_tma = p.tma_store && (!p.offsets || quad * 32 + 32 <= q.rows);
             mbar_wait_lean(&tmem_full_bar[acc], use & 1, dead, p.status);
             tc_fence_after();
-            const int row = quad * 32 + lane;
-            const bool row_ok = row < q.rows;
-            const uint32_t t_addr = tmem + acc * BN + ((uint32_t)(quad * 32) << 16);
+            if (by_tma) {
+                if (elect_one()) tma_store_wait_read();                  // the box before has left shared memory
+                __syncwarp();
+            }
 #pragma unroll
-            for (int c = 0; c < kPerWarp; ++c) {
-                const int chunk = part + 4 * c;
+            for (int c = 0; c < kChunks; ++c) {
                 float v[32];
-                const bool have = chunk < kChunks;
-                if (have) { tmem_load_32_nowait(t_addr + chunk * 32, (uint32_t*)v); tmem_load_wait(); }
-                if (c == kPerWarp - 1) {
+                tmem_load_32_nowait(t_addr + c * 32, (uint32_t*)v);
+                tmem_load_wait();
+                if (c == kChunks - 1) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&tmem_empty_bar[acc]);
                 }
-                const int col0 = q.n0 + chunk * 32;
-                if (!have || col0 >= p.N || !row_ok) continue;
+                const int col0 = first_col + c * 32;
+                if (col0 >= p.N) continue;
                 if (p.act == BIGMAC_ACT_GELU_ERF && !p.out_f32) {
                     gelu_chunk(v);
                 } else if (p.act != BIGMAC_ACT_IDENTITY) {
@@ -270,27 +309,44 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     for (int i = 0; i < 32; ++i) v[i] = act_apply(p.act, v[i]);
                 }
                 const int64_t off = (int64_t)(q.c_row + row) * p.ldc + col0;
-                if (vec_ok && col0 + 32 <= p.N) {
-                    if (p.out_f32) {
+                if (p.out_f32) {
+                    if (!row_ok) continue;
+                    if (vec_ok && col0 + 32 <= p.N) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i) st_global_32B((float*)p.C + off + 8 * i, (const uint32_t*)v + 8 * i);
                     } else {
-                        uint32_t w[16];
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+                        for (int i = 0; i < 32; ++i)
+                            if (col0 + i < p.N) ((float*)p.C)[off + i] = v[i];
+                    }
+                    continue;
+                }
+                uint32_t w[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+                if (by_tma) {
+                    stage_row<S::kCols>(box, lane, c, w);
+                } else if (row_ok) {
+                    if (vec_ok && col0 + 32 <= p.N) {
                         st_global_32B((__nv_bfloat16*)p.C + off, w);
                         st_global_32B((__nv_bfloat16*)p.C + off + 16, w + 8);
-                    }
-                } else {
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 32; ++i) {
-                        if (col0 + i >= p.N) break;
-                        if (p.out_f32) ((float*)p.C)[off + i] = v[i];
-                        else ((__nv_bfloat16*)p.C)[off + i] = __float2bfloat16(v[i]);
+                        for (int i = 0; i < 32; ++i)
+                            if (col0 + i < p.N) ((uint16_t*)p.C)[off + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
                     }
                 }
             }
+            if (by_tma && first_col < p.N) {
+                fence_async_smem();
+                __syncwarp();
+                if (elect_one()) {
+                    tma_store_2d(&map_c, box, first_col, q.c_row + quad * 32);
+                    tma_store_commit();
+                }
+            }
         }
+        if (elect_one()) tma_store_wait_read();                          // the boxes have left shared memory; the writes land before the grid ends
     }
     tc_fence_before();
     __syncthreads();
@@ -301,18 +357,23 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 }
 
 template <int BN, int STAGES>
-cudaError_t launch(const Mx4View& a, const Mx4View& w, const Mx4Params& p, int64_t max_tiles_m, cudaStream_t stream) {
-    CUtensorMap ma, ma32, mw;
+cudaError_t launch(const Mx4View& a, const Mx4View& w, Mx4Params p, int64_t max_tiles_m, cudaStream_t stream) {
+    using S = Mx4Smem<BN, STAGES>;
+    CUtensorMap ma, ma32, mw, mc;
     const uint64_t row = (uint64_t)p.K / 2;
     const uint64_t a_rows = a.offsets ? (uint64_t)a.capacity : (uint64_t)a.rows, w_rows = (uint64_t)w.rows * (w.E > 0 ? w.E : 1);
     if (!make_map_u8(&ma, a.codes, row, a_rows, row, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_map_u8(&ma32, a.codes, row, a_rows, row, 128, 32, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_map_u8(&mw, w.codes, row, w_rows, row, 128, BN, CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
+    p.tma_store = !p.out_f32 && p.ldc % 8 == 0 && (uintptr_t)p.C % 16 == 0;
+    mc = mw;
+    if (p.tma_store && !make_map(&mc, p.C, (uint64_t)p.N, (uint64_t)p.M, (uint64_t)p.ldc, S::kCols, 32,
+                                 S::kCols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
+        return cudaErrorInvalidValue;
     static PerDeviceOnce once;
     auto kernel = gemm_mx4_kernel<BN, STAGES>;
-    using S = Mx4Smem<BN, STAGES>;
-    static_assert(1024 + STAGES * S::kStage + S::kBars + (kMaxExperts + 1) * 4 <= 227 * 1024, "shared memory of a block");
+    static_assert(S::bytes(kMaxExperts) <= 227 * 1024, "shared memory of a block");
     int dev;
     if (once.needed(&dev)) {
         cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)S::bytes(kMaxExperts));
@@ -321,7 +382,7 @@ cudaError_t launch(const Mx4View& a, const Mx4View& w, const Mx4Params& p, int64
     }
     const int64_t tiles = max_tiles_m * ((p.N + BN - 1) / BN);
     const int sms = gemm_tc_sm_count();
-    return launch_chained(kernel, (int)(tiles < sms ? tiles : sms), kThreadsMx4, S::bytes(p.offsets ? p.E : 0), stream, ma, ma32, mw, p);
+    return launch_chained(kernel, (int)(tiles < sms ? tiles : sms), kThreadsMx4, S::bytes(p.offsets ? p.E : 0), stream, ma, ma32, mw, mc, p);
 }
 
 }  // namespace
@@ -335,7 +396,7 @@ cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int d
     const int64_t tiles_m = a.offsets ? a.capacity / kMx4Tile : (a.rows + kMx4Tile - 1) / kMx4Tile;
     const int sms = gemm_tc_sm_count();
     if (tiles_m * ((p.N + 127) / 128) <= sms) return launch<64, 6>(a, w, p, tiles_m, stream);
-    return launch<128, 6>(a, w, p, tiles_m, stream);
+    return launch<128, 4>(a, w, p, tiles_m, stream);
 }
 
 }  // namespace bigmac
