@@ -34,7 +34,7 @@ struct Mx4Params {
     const int32_t* offsets;                                // grouped: the caller's table
     int M, N, K, E;
     int64_t capacity;                                      // rows that A has room for (grouped)
-    int act, out_f32, tma_store;
+    int act, tma_store;
     int* status;
 };
 
@@ -64,25 +64,35 @@ __host__ __device__ constexpr uint32_t instr_desc_mx4(int bn, int half) {
            ((uint32_t)(2 * half) << 29);
 }
 
-// GELU of 32 accumulators for an output in bf16:  gelu(z) = max(z, 0) - u Q(u),  u = |z|,  Q(u) = Phi(-u) = exp(-u^2/2) G(u).  G(u) = erfcx(u / sqrt 2) / 2
-// falls smoothly from 1/2 to 0.08; the polynomial of degree 9 in u - 2.5 below is its minimax fit in relative error on [0, 5] (fitted
-// by reweighted least squares on Chebyshev nodes), 3.2e-5 in fp32, so the negative tail keeps its relative precision, too.  Behind 5 the arguments of u and
-// G stay at 5 (the term is below 2e-6 there; an infinity gives infinity or 0).  One special function and eight packed
-// instructions an element; erff takes three times the instructions, and with it the call for 131072 rows of r 256, h 1024 took 200 us.
+// GELU of 32 accumulators for an output in bf16: z Phi(z), Phi(z) = sat(1/2 + z P(z^2)).  P is the minimax fit in the error of z Phi(z) on
+// |z| <= 4.5 (reweighted least squares on Chebyshev nodes), of even degree with a positive leading coefficient, so that behind 4.5 the
+// saturating multiply-add holds Phi at 0 or 1 without a look at the argument.  z Phi(z) is off by less than 3e-6 up to 4.5 and by less
+// than 3.3e-5 everywhere (at -4.5, where it is -1.5e-5 itself): a bf16 step of 1/2 is 4e-3.  Seven instructions an element; a form that
+// keeps the relative precision of the negative tail (a polynomial times an exponential) took twelve and, at 131072 rows of r 256, h 1024,
+// 96 us, erff 142.
 __device__ __forceinline__ void gelu_chunk(float* v) {
-    constexpr float kGeluC[10] = {0.14133550226688385f, -0.045609001070261f, 0.013612025417387486f, -0.0038369703106582165f, 0.0010656173108145595f,
-                                  -0.0002591590746305883f, 4.105969856027514e-05f, -1.1991459359705914e-05f, 6.8091194407315925e-06f, -1.2926340104968403e-06f};
+    constexpr float kC[11] = {0.3989286422729492f, -0.06644835323095322f, 0.009928264655172825f, -0.0011627154890447855f, 0.00010752371599664912f, -7.800386811140925e-06f,
+                              4.3196823185098765e-07f, -1.7442022937075308e-08f, 4.790651764174925e-10f, -7.938010491981284e-12f, 5.954283154854453e-14f};
+    constexpr int kG = 8;                                  // pairs side by side, so that no multiply-add waits for the one before
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const float z0 = v[2 * i], z1 = v[2 * i + 1];
-        const f32x2_t z = pk2(z0, z1), u = pk2(fminf(fabsf(z0), 5.0f), fminf(fabsf(z1), 5.0f)), s = add2(u, pk2(-2.5f, -2.5f));
-        f32x2_t P = pk2(kGeluC[9], kGeluC[9]);
+    for (int g = 0; g < 16; g += kG) {
+        f32x2_t w[kG], P[kG];
 #pragma unroll
-        for (int k = 8; k >= 0; --k) P = fma2(P, s, pk2(kGeluC[k], kGeluC[k]));
-        float e0, e1;
-        upk2(mul2(mul2(z, z), pk2(-0.72134752f, -0.72134752f)), e0, e1);
-        const f32x2_t Q = mul2(P, pk2(fast_ex2(e0), fast_ex2(e1)));
-        upk2(fma2(mul2(u, pk2(-1.0f, -1.0f)), Q, pk2(fmaxf(z0, 0.0f), fmaxf(z1, 0.0f))), v[2 * i], v[2 * i + 1]);
+        for (int i = 0; i < kG; ++i) {
+            const f32x2_t z = pk2(v[2 * (g + i)], v[2 * (g + i) + 1]);
+            w[i] = mul2(z, z);
+            P[i] = fma2(pk2(kC[10], kC[10]), w[i], pk2(kC[9], kC[9]));
+        }
+#pragma unroll
+        for (int k = 8; k >= 0; --k)
+#pragma unroll
+            for (int i = 0; i < kG; ++i) P[i] = fma2(P[i], w[i], pk2(kC[k], kC[k]));
+#pragma unroll
+        for (int i = 0; i < kG; ++i) {
+            float &z0 = v[2 * (g + i)], &z1 = v[2 * (g + i) + 1], p0, p1;
+            upk2(P[i], p0, p1);
+            upk2(mul2(pk2(z0, z1), pk2(fma_sat(z0, p0, 0.5f), fma_sat(z1, p1, 0.5f))), z0, z1);
+        }
     }
 }
 
@@ -142,7 +152,10 @@ struct Mx4Smem {
     static constexpr size_t bytes(int E) { return 1024 + STAGES * kStage + kEpi * kBox + kBars + (size_t)(3 * E + 1) * 4; }
 };
 
-template <int BN, int STAGES>
+// What the epilogue does is fixed at compile time: with every way in one kernel its warps waited for instructions.
+enum { OUT_BF16 = 0, OUT_BF16_GELU, OUT_BF16_ACT, OUT_F32 };
+
+template <int BN, int STAGES, int OUT>
 __global__ void __launch_bounds__(kThreadsMx4, 1)
 gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32, const __grid_constant__ CUtensorMap map_w,
                 const __grid_constant__ CUtensorMap map_c, const Mx4Params p) {
@@ -272,7 +285,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         const uint32_t acc = (uint32_t)(warp - 2) >> 3;
         constexpr int kChunks = S::kCols / 32;
         uint8_t* box = boxes_c + (warp - 2) * S::kBox;
-        const int esz = p.out_f32 ? 4 : 2;
+        constexpr int esz = OUT == OUT_F32 ? 4 : 2;
         const bool vec_ok = (p.ldc * esz) % 32 == 0 && (uintptr_t)p.C % 32 == 0;
         const uint32_t t_addr = tmem + acc * BN + ((uint32_t)(quad * 32) << 16) + half * S::kCols;
         uint32_t use = 0;
@@ -302,14 +315,14 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 }
                 const int col0 = first_col + c * 32;
                 if (col0 >= p.N) continue;
-                if (p.act == BIGMAC_ACT_GELU_ERF && !p.out_f32) {
+                if (OUT == OUT_BF16_GELU) {
                     gelu_chunk(v);
-                } else if (p.act != BIGMAC_ACT_IDENTITY) {
+                } else if (OUT == OUT_BF16_ACT || (OUT == OUT_F32 && p.act != BIGMAC_ACT_IDENTITY)) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = act_apply(p.act, v[i]);
                 }
                 const int64_t off = (int64_t)(q.c_row + row) * p.ldc + col0;
-                if (p.out_f32) {
+                if constexpr (OUT == OUT_F32) {
                     if (!row_ok) continue;
                     if (vec_ok && col0 + 32 <= p.N) {
 #pragma unroll
@@ -319,8 +332,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         for (int i = 0; i < 32; ++i)
                             if (col0 + i < p.N) ((float*)p.C)[off + i] = v[i];
                     }
-                    continue;
-                }
+                } else {
                 uint32_t w[16];
 #pragma unroll
                 for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
@@ -335,6 +347,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                         for (int i = 0; i < 32; ++i)
                             if (col0 + i < p.N) ((uint16_t*)p.C)[off + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
                     }
+                }
                 }
             }
             if (by_tma && first_col < p.N) {
@@ -356,7 +369,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     }
 }
 
-template <int BN, int STAGES>
+template <int BN, int STAGES, int OUT>
 cudaError_t launch(const Mx4View& a, const Mx4View& w, Mx4Params p, int64_t max_tiles_m, cudaStream_t stream) {
     using S = Mx4Smem<BN, STAGES>;
     CUtensorMap ma, ma32, mw, mc;
@@ -366,13 +379,13 @@ cudaError_t launch(const Mx4View& a, const Mx4View& w, Mx4Params p, int64_t max_
         !make_map_u8(&ma32, a.codes, row, a_rows, row, 128, 32, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_map_u8(&mw, w.codes, row, w_rows, row, 128, BN, CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
-    p.tma_store = !p.out_f32 && p.ldc % 8 == 0 && (uintptr_t)p.C % 16 == 0;
+    p.tma_store = OUT != OUT_F32 && p.ldc % 8 == 0 && (uintptr_t)p.C % 16 == 0;
     mc = mw;
     if (p.tma_store && !make_map(&mc, p.C, (uint64_t)p.N, (uint64_t)p.M, (uint64_t)p.ldc, S::kCols, 32,
                                  S::kCols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
         return cudaErrorInvalidValue;
     static PerDeviceOnce once;
-    auto kernel = gemm_mx4_kernel<BN, STAGES>;
+    auto kernel = gemm_mx4_kernel<BN, STAGES, OUT>;
     static_assert(S::bytes(kMaxExperts) <= 227 * 1024, "shared memory of a block");
     int dev;
     if (once.needed(&dev)) {
@@ -385,6 +398,14 @@ cudaError_t launch(const Mx4View& a, const Mx4View& w, Mx4Params p, int64_t max_
     return launch_chained(kernel, (int)(tiles < sms ? tiles : sms), kThreadsMx4, S::bytes(p.offsets ? p.E : 0), stream, ma, ma32, mw, mc, p);
 }
 
+template <int BN, int STAGES>
+cudaError_t launch_out(const Mx4View& a, const Mx4View& w, const Mx4Params& p, int dtype, int64_t max_tiles_m, cudaStream_t stream) {
+    if (dtype == BIGMAC_F32) return launch<BN, STAGES, OUT_F32>(a, w, p, max_tiles_m, stream);
+    if (p.act == BIGMAC_ACT_IDENTITY) return launch<BN, STAGES, OUT_BF16>(a, w, p, max_tiles_m, stream);
+    if (p.act == BIGMAC_ACT_GELU_ERF) return launch<BN, STAGES, OUT_BF16_GELU>(a, w, p, max_tiles_m, stream);
+    return launch<BN, STAGES, OUT_BF16_ACT>(a, w, p, max_tiles_m, stream);
+}
+
 }  // namespace
 
 cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int dtype, void* c, int64_t ldc, int* status, cudaStream_t stream) {
@@ -392,11 +413,11 @@ cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int d
     Mx4Params p{};
     p.C = c; p.ldc = ldc; p.sa = a.scales; p.sw = w.scales; p.offsets = a.offsets;
     p.M = a.rows; p.N = w.rows; p.K = a.K; p.E = a.E; p.capacity = a.capacity;
-    p.act = act; p.out_f32 = dtype == BIGMAC_F32; p.status = status;
+    p.act = act; p.status = status;
     const int64_t tiles_m = a.offsets ? a.capacity / kMx4Tile : (a.rows + kMx4Tile - 1) / kMx4Tile;
     const int sms = gemm_tc_sm_count();
-    if (tiles_m * ((p.N + 127) / 128) <= sms) return launch<64, 6>(a, w, p, tiles_m, stream);
-    return launch<128, 4>(a, w, p, tiles_m, stream);
+    if (tiles_m * ((p.N + 127) / 128) <= sms) return launch_out<64, 6>(a, w, p, dtype, tiles_m, stream);
+    return launch_out<128, 4>(a, w, p, dtype, tiles_m, stream);
 }
 
 }  // namespace bigmac

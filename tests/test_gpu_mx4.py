@@ -108,6 +108,9 @@ def _check_product(got, a, w, act, dtype):
     K = a.shape[1]
     want = _act(z, act)
     err = 1.13 * (K / 64 + 2) * 2.0 ** -23 * S + (np.abs(z) * 2.0 ** -20 if act in (1, 2) else 0)
+    # GELU of a bf16 output is a polynomial under saturation, off by less than 3.3e-5: its minimax error and its fp32 evaluation, looked at on
+    # two million points of [-12, 12]; outside Phi is 0 or 1 and so is the polynomial's sum
+    err += 3.3e-5 if act == 1 and dtype == torch.bfloat16 else 0
     err += np.abs(want) * torch.finfo(dtype).eps / 2 * 1.01
     diff = np.abs(got.double().cpu().numpy() - want)
     assert (diff <= err).all(), (float((diff - err).max()), float((diff / np.maximum(np.abs(want), 1e-30)).max()))
