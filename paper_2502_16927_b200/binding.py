@@ -371,16 +371,20 @@ def _dense(t: torch.Tensor, name: str, here: int) -> int:
     return t.data_ptr()
 
 
-def _matrix(t: torch.Tensor, name: str, here: int):
-    """(address, row stride) of a matrix with dense rows."""
-    if t.get_device() == here and t.dim() == 2:
-        rows, columns = t.shape
+def _matrix(t: torch.Tensor, shape, name: str, here: int):
+    """(address, row stride) of a matrix with dense rows; shape is t.shape."""
+    if t.get_device() == here and len(shape) == 2:
         if t.is_contiguous():
-            return t.data_ptr(), columns
+            return t.data_ptr(), shape[1]
+        rows, columns = shape
         ld, step = t.stride()
         if (step == 1 or columns == 1) and (ld >= columns or rows == 1):
             return t.data_ptr(), max(ld, columns)
     raise ValueError(f"{name}: a matrix with dense rows that do not overlap, on the current device, cuda:{here}, is needed")
+
+
+def _new(rows: int, columns: int, dtype, device) -> torch.Tensor:
+    return torch.empty_strided((rows, columns), (columns, 1), dtype=dtype, device=device)       # half the time of torch.empty
 
 
 def _vector(t: Optional[torch.Tensor], name: str, n: int, here: int) -> int:
@@ -410,41 +414,41 @@ _NOTHING = (0, 0)
 _NO_BACKWARD = 14 * (0,)
 
 
-def _rows_like(t: Optional[torch.Tensor], name: str, x: torch.Tensor, here: int):
-    """(address, row stride) of a matrix of x's shape and type, (0, 0) where there is none."""
+def _rows_like(t: Optional[torch.Tensor], name: str, shape, dtype, here: int):
+    """(address, row stride) of a matrix of this shape and type, (0, 0) where there is none."""
     if t is None:
         return _NOTHING
-    if t.dtype is not x.dtype or t.shape != x.shape:
-        raise ValueError(f"{name}: {tuple(x.shape)} of {x.dtype} is needed, not {tuple(t.shape)} of {t.dtype}")
-    return _matrix(t, name, here)
+    if t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{name}: {tuple(shape)} of {dtype} is needed, not {tuple(t.shape)} of {t.dtype}")
+    return _matrix(t, shape, name, here)
 
 
-def _gate_kind(gate, x, gate_kind) -> int:
+def _gate_kind(gate, T: int, gate_kind) -> int:
     """The gate's kind by its shape; a vector as long as both T and d is one factor a token unless gate_kind says otherwise."""
     if gate.dim() == 2:
         kind = BIGMAC_GATE_FULL
-    elif gate_kind in (BIGMAC_GATE_TOKEN, BIGMAC_GATE_CHANNEL):
+    elif gate_kind == BIGMAC_GATE_TOKEN or gate_kind == BIGMAC_GATE_CHANNEL:
         return gate_kind
     else:
-        kind = BIGMAC_GATE_TOKEN if gate.shape[0] == x.shape[0] else BIGMAC_GATE_CHANNEL
+        kind = BIGMAC_GATE_TOKEN if gate.shape[0] == T else BIGMAC_GATE_CHANNEL
     if gate_kind is not None and kind != gate_kind:
         raise ValueError(f"gate_kind {gate_kind}: a gate of shape {tuple(gate.shape)}")
     return kind
 
 
-def _joint(x, y, gate, gate_kind, post, pre, residual_scale, here):
-    """The members of bigmac_residual_norm_t that forward and backward share, up to `gate`, and the gate's kind."""
-    at = _matrix(x, "x", here)
-    T, d = x.shape
+def _joint(x, shape, dtype, y, gate, gate_kind, post, pre, residual_scale, here):
+    """The members of bigmac_residual_norm_t that forward and backward share, up to `gate`."""
+    at, ld = _matrix(x, shape, "x", here)
+    T, d = shape
     kind, g = BIGMAC_GATE_NONE, _NOTHING
     if gate is not None:
-        kind = _gate_kind(gate, x, gate_kind)
-        g = _rows_like(gate, "gate", x, here) if kind == BIGMAC_GATE_FULL else (_vector(gate, "gate", T if kind == BIGMAC_GATE_TOKEN else d, here), 0)
-    post_kind, w_post, b_post, post_eps = post or _NO_NORM
-    pre_kind, w_pre, b_pre, pre_eps = pre or _NO_NORM
-    return (d, _dtype(x.dtype), post_kind, pre_kind, kind, post_eps, pre_eps, residual_scale, _vector(w_post, "post.weight", d, here),
-            _vector(b_post, "post.bias", d, here), _vector(w_pre, "pre.weight", d, here), _vector(b_pre, "pre.bias", d, here), *at,
-            *_rows_like(y, "y", x, here), *g), kind
+        kind = _gate_kind(gate, T, gate_kind)
+        g = _rows_like(gate, "gate", shape, dtype, here) if kind == BIGMAC_GATE_FULL else (_vector(gate, "gate", T if kind == BIGMAC_GATE_TOKEN else d, here), 0)
+    post_kind, w_post, b_post, post_eps = _NO_NORM if post is None else post
+    pre_kind, w_pre, b_pre, pre_eps = _NO_NORM if pre is None else pre
+    return (d, _dtype(dtype), post_kind, pre_kind, kind, post_eps, pre_eps, residual_scale, _vector(w_post, "post.weight", d, here),
+            _vector(b_post, "post.bias", d, here), _vector(w_pre, "pre.weight", d, here), _vector(b_pre, "pre.bias", d, here), at, ld,
+            *_rows_like(y, "y", shape, dtype, here), *g)
 
 
 def residual_norm_forward(x: torch.Tensor, y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, post: Optional[Norm] = None,
@@ -452,17 +456,26 @@ def residual_norm_forward(x: torch.Tensor, y: Optional[torch.Tensor] = None, gat
                           r: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None):
     """r = residual_scale x + gate N_post(y) and n = N_pre(r) (bigmac_residual_norm_forward): (r, n, stats), n None without `pre`, stats (for
     the backward) None unless `training`.  gate: [T] or [d] fp32, or [T, d].  r and n may be given, in place too (r is x, n is y)."""
-    here = _here()
-    members, _ = _joint(x, y, gate, gate_kind, post, pre, residual_scale, here)
-    T, d = x.shape
+    here, shape, dtype = _here(), x.shape, x.dtype
+    members = _joint(x, shape, dtype, y, gate, gate_kind, post, pre, residual_scale, here)
+    T, d = shape
     if r is None:
         r = torch.empty_like(x)
+        r_at, r_ld = r.data_ptr(), d
+    else:
+        r_at, r_ld = _rows_like(r, "r", shape, dtype, here)
     if n is None and members[3] != BIGMAC_NORM_NONE:
         n = torch.empty_like(x)
-    stats = torch.empty((T, 4), dtype=torch.float32, device=x.device) if training else None
-    q = _RESIDUAL_NORM.pack(*members, *_rows_like(r, "r", x, here), *_rows_like(n, "n", x, here), 0 if stats is None else stats.data_ptr(), *_NO_BACKWARD)
+        n_at, n_ld = n.data_ptr(), d
+    else:
+        n_at, n_ld = _rows_like(n, "n", shape, dtype, here)
+    stats = _new(T, 4, torch.float32, x.device) if training else None
+    q = _RESIDUAL_NORM.pack(*members, r_at, r_ld, n_at, n_ld, 0 if stats is None else stats.data_ptr(), *_NO_BACKWARD)
     _check(lib().bigmac_residual_norm_forward(q, T, _stream()), "bigmac_residual_norm_forward")
     return r, n, stats
+
+
+_residual_norm_scratch = {}                             # bytes by (device, T, d): a function of the sizes and the card
 
 
 def residual_norm_backward(x, y, gate, post, pre, dr, dn, stats, G: Optional[Dict[str, torch.Tensor]] = None, residual_scale: float = 1.0,
@@ -470,30 +483,44 @@ def residual_norm_backward(x, y, gate, post, pre, dr, dn, stats, G: Optional[Dic
     """Gradients of sum(r dr) + sum(n dn) (bigmac_residual_norm_backward): (dx, dy, dgate), None for what was not in the call.  G holds
     fp32 buffers for the gradients of the parameters, any of dw_post, db_post, dw_pre, db_pre and, for a gate [d], dgate (returned,
     too); with `accumulate` they are added to.  dr or dn may be None."""
-    here = _here()
-    members, kind = _joint(x, y, gate, gate_kind, post, pre, residual_scale, here)
-    G, (T, d) = G or {}, x.shape
+    here, shape, dtype = _here(), x.shape, x.dtype
+    members = _joint(x, shape, dtype, y, gate, gate_kind, post, pre, residual_scale, here)
+    T, d = shape
+    kind = members[4]
     dx = torch.empty_like(x)
-    dy = None if y is None else torch.empty_like(x)
+    dy_at, dy_ld, dy = 0, 0, None
+    if y is not None:
+        dy = torch.empty_like(x)
+        dy_at, dy_ld = dy.data_ptr(), d
+    grads = [0, 0, 0, 0]
+    if G:
+        get = G.get
+        grads = [_vector(get("dw_post"), "dw_post", d, here), _vector(get("db_post"), "db_post", d, here),
+                 _vector(get("dw_pre"), "dw_pre", d, here), _vector(get("db_pre"), "db_pre", d, here)]
+    dgate, dg_at, dg_ld = None, 0, 0
     if kind == BIGMAC_GATE_CHANNEL:
-        dgate = G.get("dgate")
-        dg = (_vector(dgate, "dgate", d, here), 0)
-    elif kind == BIGMAC_GATE_NONE:
-        dgate, dg = None, _NOTHING
-    else:
+        dgate = G.get("dgate") if G else None
+        dg_at = _vector(dgate, "dgate", d, here)
+    elif kind != BIGMAC_GATE_NONE:
         dgate = torch.empty_like(gate)
-        dg = (dgate.data_ptr(), d)
+        dg_at, dg_ld = dgate.data_ptr(), d
     if stats is None or stats.dtype is not torch.float32 or stats.shape != (T, 4):
         raise ValueError("stats: those of a training forward of the same rows")
-    q = _RESIDUAL_NORM.pack(*members, 0, 0, 0, 0, _dense(stats, "stats", here), *_rows_like(dr, "dr", x, here), *_rows_like(dn, "dn", x, here),
-                            dx.data_ptr(), d, *(_NOTHING if dy is None else (dy.data_ptr(), d)), *dg, _vector(G.get("dw_post"), "dw_post", d, here),
-                            _vector(G.get("db_post"), "db_post", d, here), _vector(G.get("dw_pre"), "dw_pre", d, here),
-                            _vector(G.get("db_pre"), "db_pre", d, here))
-    need = C.c_size_t()
-    _check(lib().bigmac_residual_norm_scratch_bytes(q, T, C.byref(need)), "bigmac_residual_norm_scratch_bytes")
-    scratch = torch.empty(need.value, dtype=torch.uint8, device=x.device) if need.value else None
-    _check(lib().bigmac_residual_norm_backward(q, T, int(accumulate), None if scratch is None else scratch.data_ptr(), need.value, _stream()),
-           "bigmac_residual_norm_backward")
+    q = _RESIDUAL_NORM.pack(*members, 0, 0, 0, 0, _dense(stats, "stats", here), *_rows_like(dr, "dr", shape, dtype, here),
+                            *_rows_like(dn, "dn", shape, dtype, here), dx.data_ptr(), d, dy_at, dy_ld, dg_at, dg_ld, *grads)
+    scratch, at, need = None, None, 0
+    if any(grads) or (kind == BIGMAC_GATE_CHANNEL and dg_at):
+        need = _residual_norm_scratch.get((here, T, d))
+        if need is None:
+            size = C.c_size_t()
+            _check(lib().bigmac_residual_norm_scratch_bytes(q, T, C.byref(size)), "bigmac_residual_norm_scratch_bytes")
+            if len(_residual_norm_scratch) >= 4096:
+                _residual_norm_scratch.clear()
+            need = _residual_norm_scratch[here, T, d] = size.value
+        if need:
+            scratch = torch.empty_strided((need,), (1,), dtype=torch.uint8, device=x.device)
+            at = scratch.data_ptr()
+    _check(lib().bigmac_residual_norm_backward(q, T, accumulate, at, need, _stream()), "bigmac_residual_norm_backward")
     return dx, dy, dgate
 
 
@@ -543,9 +570,9 @@ def _offsets(t: torch.Tensor, here: int) -> int:
 def mx4_quantize(x: torch.Tensor, offsets: Optional[torch.Tensor] = None, slot_of_row: Optional[torch.Tensor] = None, k: int = 1) -> Mx4:
     """Rows of x to 4 bits (bigmac_mx4_quantize).  With `offsets` (int32 [E + 1], of a routing) grouped by expert; with `slot_of_row`
     row i is x[slot_of_row[i] // k]: the dispatch."""
-    here = _here()
-    ptr, ld = _matrix(x, "x", here)
-    x_rows, K = x.shape
+    here, shape = _here(), x.shape
+    ptr, ld = _matrix(x, shape, "x", here)
+    x_rows, K = shape
     rows, slots, E, table = x_rows, None, 0, None
     if K == 0 or K % 32:
         raise ValueError(f"K = {K}: blocks of 32 columns")
@@ -558,8 +585,9 @@ def mx4_quantize(x: torch.Tensor, offsets: Optional[torch.Tensor] = None, slot_o
         E, table = _offsets(offsets, here), offsets.data_ptr()
         stored = _mx4_stored(rows, E)
     device = x.device
-    codes = torch.empty((stored, K // 2), dtype=torch.uint8, device=device)
-    scales = torch.empty((-(-stored // 128), -(-K // 128), 512), dtype=torch.uint8, device=device)
+    codes = _new(stored, K // 2, torch.uint8, device)
+    row_tiles, k_tiles = -(-stored // 128), -(-K // 128)
+    scales = torch.empty_strided((row_tiles, k_tiles, 512), (k_tiles * 512, 512, 1), dtype=torch.uint8, device=device)
     q = bigmac_mx4_t(codes.data_ptr(), scales.data_ptr(), rows, K, E, table)
     _check(lib().bigmac_mx4_quantize(ptr, _dtype(x.dtype), x_rows, ld, slots, k, C.byref(q), _stream()), "bigmac_mx4_quantize")
     return Mx4(codes, scales, offsets, rows)
@@ -568,11 +596,11 @@ def mx4_quantize(x: torch.Tensor, offsets: Optional[torch.Tensor] = None, slot_o
 def _output(out, rows: int, columns: int, dtype, device, here: int):
     """The result's matrix: (tensor, address, row stride, bigmac_dtype_t)."""
     if out is None:
-        out = torch.empty((rows, columns), dtype=dtype, device=device)
+        out = _new(rows, columns, dtype, device)
         return out, out.data_ptr(), columns, _dtype(dtype)
     if out.shape != (rows, columns):
         raise ValueError(f"out has shape {tuple(out.shape)}, not {(rows, columns)}")
-    return (out, *_matrix(out, "out", here), _dtype(out.dtype))
+    return (out, *_matrix(out, out.shape, "out", here), _dtype(out.dtype))
 
 
 def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:

@@ -35,6 +35,7 @@ struct Mx4Params {
     int M, N, K, E;
     int64_t capacity;                                      // rows that A has room for (grouped)
     int act, tma_store;
+    int box_rows;                                          // of A's codes: a tile with few rows loads few
     int* status;
 };
 
@@ -157,7 +158,7 @@ enum { OUT_BF16 = 0, OUT_BF16_GELU, OUT_BF16_ACT, OUT_F32 };
 
 template <int BN, int STAGES, int OUT>
 __global__ void __launch_bounds__(kThreadsMx4, 1)
-gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_a32, const __grid_constant__ CUtensorMap map_w,
+gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_w,
                 const __grid_constant__ CUtensorMap map_c, const Mx4Params p) {
     using S = Mx4Smem<BN, STAGES>;
     constexpr uint32_t kSfCol = 2 * BN;                                  // scale bytes behind them: A's 8 columns, then W's
@@ -177,7 +178,6 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 32) {
         prefetch_tensormap(&map_a);
-        prefetch_tensormap(&map_a32);
         prefetch_tensormap(&map_w);
         prefetch_tensormap(&map_c);
     }
@@ -222,8 +222,8 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const uint8_t* sa = p.sa + (int64_t)walk.mt * ktiles * kSfTile;
                 const uint8_t* sw = p.sw + ((int64_t)q.expert * w_row_tiles + wt) * ktiles * kSfTile;
                 const int w_tiles = min(S::kWTiles, w_row_tiles - wt);
-                const int boxes = q.rows > 96 ? 0 : (q.rows + 31) / 32;  // of 32 rows; 0: all 128 in one
-                const uint32_t a_bytes = boxes ? boxes * 32 * 128 : kABytes;
+                const int boxes = (q.rows + p.box_rows - 1) / p.box_rows;
+                const uint32_t a_bytes = boxes * p.box_rows * 128;
                 for (int kb = 0; kb < num_kb; ++kb, s = (s + 1 == STAGES ? 0 : s + 1), phase ^= (s == 0)) {
                     mbar_wait_lean(&empty_bar[s], phase, dead, p.status);
                     const uint32_t sf = kSfTile * min(2, ktiles - 2 * kb);
@@ -231,8 +231,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     uint8_t* a = smem + s * S::kStage;
                     uint8_t* b = a + kABytes;
                     uint8_t* f = b + S::kBBytes;
-                    if (boxes) for (int i = 0; i < boxes; ++i) tma_load_2d(a + i * 32 * 128, &map_a32, &full_bar[s], kb * 128, a_row + 32 * i);
-                    else tma_load_2d(a, &map_a, &full_bar[s], kb * 128, a_row);
+                    for (int i = 0; i < boxes; ++i) tma_load_2d(a + i * p.box_rows * 128, &map_a, &full_bar[s], kb * 128, a_row + i * p.box_rows);
                     tma_load_2d(b, &map_w, &full_bar[s], kb * 128, q.expert * p.N + n0);
                     bulk_load(f, sa + kb * 2 * kSfTile, sf, &full_bar[s]);
                     for (int i = 0; i < w_tiles; ++i)
@@ -372,11 +371,11 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 template <int BN, int STAGES, int OUT>
 cudaError_t launch(const Mx4View& a, const Mx4View& w, Mx4Params p, int64_t max_tiles_m, cudaStream_t stream) {
     using S = Mx4Smem<BN, STAGES>;
-    CUtensorMap ma, ma32, mw, mc;
+    CUtensorMap ma, mw, mc;
     const uint64_t row = (uint64_t)p.K / 2;
     const uint64_t a_rows = a.offsets ? (uint64_t)a.capacity : (uint64_t)a.rows, w_rows = (uint64_t)w.rows * (w.E > 0 ? w.E : 1);
-    if (!make_map_u8(&ma, a.codes, row, a_rows, row, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
-        !make_map_u8(&ma32, a.codes, row, a_rows, row, 128, 32, CU_TENSOR_MAP_SWIZZLE_128B) ||
+    p.box_rows = a.rows <= (p.offsets ? 96 * (int64_t)p.E : 96) ? 32 : 128;
+    if (!make_map_u8(&ma, a.codes, row, a_rows, row, 128, p.box_rows, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_map_u8(&mw, w.codes, row, w_rows, row, 128, BN, CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
     p.tma_store = OUT != OUT_F32 && p.ldc % 8 == 0 && (uintptr_t)p.C % 16 == 0;
@@ -395,7 +394,7 @@ cudaError_t launch(const Mx4View& a, const Mx4View& w, Mx4Params p, int64_t max_
     }
     const int64_t tiles = max_tiles_m * ((p.N + BN - 1) / BN);
     const int sms = gemm_tc_sm_count();
-    return launch_chained(kernel, (int)(tiles < sms ? tiles : sms), kThreadsMx4, S::bytes(p.offsets ? p.E : 0), stream, ma, ma32, mw, mc, p);
+    return launch_chained(kernel, (int)(tiles < sms ? tiles : sms), kThreadsMx4, S::bytes(p.offsets ? p.E : 0), stream, ma, mw, mc, p);
 }
 
 template <int BN, int STAGES>
