@@ -149,6 +149,7 @@ int bigmac_mx4_quantize(const void* x, int32_t dtype, int32_t x_rows, int64_t ld
     if (!dtype_ok(dtype) || x_rows < 0 || ld < out->K || (ld * esize_of(dtype)) % 16 || !is_aligned(x, 16) || !is_aligned(slot_of_row, 4) ||
         (slot_of_row ? k < 1 : x_rows != out->rows) || (x_rows > 0 && !x))
         return BIGMAC_ERR_INVALID_ARG;
+    if (ld > 0x7fffffff) return BIGMAC_ERR_UNSUPPORTED;
     return launch_mx4_quantize(x, dtype, ld, slot_of_row, k, x_rows, view_of(out), (cudaStream_t)stream) == cudaSuccess ? BIGMAC_OK : BIGMAC_ERR_CUDA;
 }
 
@@ -156,6 +157,7 @@ int bigmac_mx4_dequantize(const bigmac_mx4_t* q, void* y, int32_t dtype, int64_t
     const int s = check_mx4(q, false);
     if (s != BIGMAC_OK) return s;
     if (!dtype_ok(dtype) || ld < q->K || (ld * esize_of(dtype)) % 16 || !is_aligned(y, 16) || (q->rows > 0 && !y)) return BIGMAC_ERR_INVALID_ARG;
+    if (ld > 0x7fffffff) return BIGMAC_ERR_UNSUPPORTED;
     return launch_mx4_dequantize(view_of(q), y, dtype, ld, (cudaStream_t)stream) == cudaSuccess ? BIGMAC_OK : BIGMAC_ERR_CUDA;
 }
 
