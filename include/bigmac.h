@@ -384,6 +384,9 @@ int bigmac_mx4_dequantize(const bigmac_mx4_t *q, void *y, int32_t dtype, int64_t
  * the caller's order, ldc elements apart; rows in no segment are left as they are. */
 int bigmac_mx4_matmul(const bigmac_mx4_t *a, const bigmac_mx4_t *w, int32_t act, int32_t dtype, void *c, int64_t ldc,
                       void *stream);
+/* The same with a result in 4 bits, quantised as by bigmac_mx4_quantize from the fp32 values (not rounded to bf16 first): out
+ * has a's rows, K = w->rows (a multiple of 32) and, grouped, a's E and the same offsets: the input of a next product. */
+int bigmac_mx4_matmul_mx4(const bigmac_mx4_t *a, const bigmac_mx4_t *w, int32_t act, const bigmac_mx4_t *out, void *stream);
 
 /* bigmac_route for callers that cannot provide scratch memory.  (The paper has no counterpart: this is
  * a deployment variant of the routing step, not part of the method.)

@@ -124,6 +124,8 @@ def lib() -> C.CDLL:
         L.bigmac_mx4_quantize.argtypes = [vp, i32, i32, i64, vp, i32, Q, vp]
         L.bigmac_mx4_dequantize.argtypes = [Q, vp, i32, i64, vp]
         L.bigmac_mx4_matmul.argtypes = [Q, Q, i32, i32, vp, i64, vp]
+        L.bigmac_mx4_matmul_mx4.argtypes = [Q, Q, i32, Q, vp]
+        L.bigmac_mx4_matmul_mx4.restype = C.c_int
         L.bigmac_residual_norm_forward.argtypes = [vp, i32, vp]
         L.bigmac_residual_norm_scratch_bytes.argtypes = [vp, i32, C.POINTER(sz)]
         L.bigmac_residual_norm_backward.argtypes = [vp, i32, C.c_int, vp, sz, vp]
@@ -584,10 +586,7 @@ def mx4_quantize(x: torch.Tensor, offsets: Optional[torch.Tensor] = None, slot_o
     if offsets is not None:
         E, table = _offsets(offsets, here), offsets.data_ptr()
         stored = _mx4_stored(rows, E)
-    device = x.device
-    codes = _new(stored, K // 2, torch.uint8, device)
-    row_tiles, k_tiles = -(-stored // 128), -(-K // 128)
-    scales = torch.empty_strided((row_tiles, k_tiles, 512), (k_tiles * 512, 512, 1), dtype=torch.uint8, device=device)
+    codes, scales = _empty_mx4(stored, K, x.device)
     q = bigmac_mx4_t(codes.data_ptr(), scales.data_ptr(), rows, K, E, table)
     _check(lib().bigmac_mx4_quantize(ptr, _dtype(x.dtype), x_rows, ld, slots, k, C.byref(q), _stream()), "bigmac_mx4_quantize")
     return Mx4(codes, scales, offsets, rows)
@@ -619,6 +618,24 @@ def mx4_matmul(a: Mx4, w: Mx4, act: int = 3, dtype: torch.dtype = torch.bfloat16
     out, ptr, ld, kind = _output(out, ca.rows, cw.rows, dtype, a.codes.device, here)
     _check(lib().bigmac_mx4_matmul(C.byref(ca), C.byref(cw), act, kind, ptr, ld, _stream()), "bigmac_mx4_matmul")
     return out
+
+
+def _empty_mx4(stored: int, K: int, device):
+    k_tiles = -(-K // 128)
+    return (_new(stored, K // 2, torch.uint8, device),
+            torch.empty_strided((-(-stored // 128), k_tiles, 512), (k_tiles * 512, 512, 1), dtype=torch.uint8, device=device))
+
+
+def mx4_matmul_mx4(a: Mx4, w: Mx4, act: int = 3) -> Mx4:
+    """act(a w^T) in 4 bits (bigmac_mx4_matmul_mx4), with a's rows: the input of a next product."""
+    here = _here()
+    ca, cw = _mx4(a, here), _mx4(w, here)
+    if cw.rows == 0 or cw.rows % 32:
+        raise ValueError(f"{cw.rows} columns: blocks of 32")
+    codes, scales = _empty_mx4(a.codes.shape[0], cw.rows, a.codes.device)
+    out = bigmac_mx4_t(codes.data_ptr(), scales.data_ptr(), ca.rows, cw.rows, ca.E, ca.offsets)
+    _check(lib().bigmac_mx4_matmul_mx4(C.byref(ca), C.byref(cw), act, C.byref(out), _stream()), "bigmac_mx4_matmul_mx4")
+    return Mx4(codes, scales, a.offsets, a.rows)
 
 
 # ---- a small convenience wrapper: owns the handle and the workspaces ------------------------------------

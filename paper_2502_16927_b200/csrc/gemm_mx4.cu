@@ -31,6 +31,7 @@ struct Mx4Params {
     void* C;
     int64_t ldc;
     const uint8_t *sa, *sw;                                // scale bytes
+    uint8_t *out_codes, *out_scales;                       // OUT_MX4: the result's
     const int32_t* offsets;                                // grouped: the caller's table
     int M, N, K, E;
     int64_t capacity;                                      // rows that A has room for (grouped)
@@ -153,8 +154,29 @@ struct Mx4Smem {
     static constexpr size_t bytes(int E) { return 1024 + STAGES * kStage + kEpi * kBox + kBars + (size_t)(3 * E + 1) * 4; }
 };
 
+// 32 columns of a row are a block of the result in 4 bits: its scale and codes from the fp32 numbers, without a rounding between.
+__device__ __forceinline__ void store_block(const Mx4Params& p, float* v, int row, int block) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = max_nan(top, fabsf(v[i]));
+    const uint32_t s = mx4_scale_byte(top);
+    uint32_t c[4] = {0u, 0u, 0u, 0u};
+    if (s != 255u) {
+        const f32x2_t factor = mx4_factor2(s);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) upk2(mul2(pk2(v[2 * i], v[2 * i + 1]), factor), v[2 * i], v[2 * i + 1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = mx4_e2m1x8(v + 8 * i);
+    }
+    *(uint4*)(p.out_codes + (int64_t)row * (p.N / 2) + block * 16) = make_uint4(c[0], c[1], c[2], c[3]);
+    uint8_t* at = p.out_scales + mx4_scale_at(row, block, mx4_ktiles(p.N));
+    *at = (uint8_t)s;
+    if (block + 1 == p.N / 32)
+        for (int b = block + 1; b & 3; ++b) *++at = 0;                   // behind the last block of the row
+}
+
 // What the epilogue does is fixed at compile time: with every way in one kernel its warps waited for instructions.
-enum { OUT_BF16 = 0, OUT_BF16_GELU, OUT_BF16_ACT, OUT_F32 };
+enum { OUT_BF16 = 0, OUT_BF16_GELU, OUT_BF16_ACT, OUT_F32, OUT_MX4_GELU, OUT_MX4 };
 
 template <int BN, int STAGES, int OUT>
 __global__ void __launch_bounds__(kThreadsMx4, 1)
@@ -285,6 +307,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         constexpr int kChunks = S::kCols / 32;
         uint8_t* box = boxes_c + (warp - 2) * S::kBox;
         constexpr int esz = OUT == OUT_F32 ? 4 : 2;
+        constexpr bool kMx4Out = OUT == OUT_MX4 || OUT == OUT_MX4_GELU;
         const bool vec_ok = (p.ldc * esz) % 32 == 0 && (uintptr_t)p.C % 32 == 0;
         const uint32_t t_addr = tmem + acc * BN + ((uint32_t)(quad * 32) << 16) + half * S::kCols;
         uint32_t use = 0;
@@ -314,11 +337,15 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 }
                 const int col0 = first_col + c * 32;
                 if (col0 >= p.N) continue;
-                if (OUT == OUT_BF16_GELU) {
+                if (OUT == OUT_BF16_GELU || OUT == OUT_MX4_GELU) {
                     gelu_chunk(v);
-                } else if (OUT == OUT_BF16_ACT || (OUT == OUT_F32 && p.act != BIGMAC_ACT_IDENTITY)) {
+                } else if (OUT == OUT_BF16_ACT || ((OUT == OUT_F32 || OUT == OUT_MX4) && p.act != BIGMAC_ACT_IDENTITY)) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) v[i] = act_apply(p.act, v[i]);
+                }
+                if constexpr (kMx4Out) {
+                    if (row_ok) store_block(p, v, walk.mt * kMx4Tile + row, col0 / 32);
+                    continue;
                 }
                 const int64_t off = (int64_t)(q.c_row + row) * p.ldc + col0;
                 if constexpr (OUT == OUT_F32) {
@@ -378,7 +405,7 @@ cudaError_t launch(const Mx4View& a, const Mx4View& w, Mx4Params p, int64_t max_
     if (!make_map_u8(&ma, a.codes, row, a_rows, row, 128, p.box_rows, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_map_u8(&mw, w.codes, row, w_rows, row, 128, BN, CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
-    p.tma_store = OUT != OUT_F32 && p.ldc % 8 == 0 && (uintptr_t)p.C % 16 == 0;
+    p.tma_store = OUT <= OUT_BF16_ACT && p.ldc % 8 == 0 && (uintptr_t)p.C % 16 == 0;
     mc = mw;
     if (p.tma_store && !make_map(&mc, p.C, (uint64_t)p.N, (uint64_t)p.M, (uint64_t)p.ldc, S::kCols, 32,
                                  S::kCols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
@@ -399,6 +426,8 @@ cudaError_t launch(const Mx4View& a, const Mx4View& w, Mx4Params p, int64_t max_
 
 template <int BN, int STAGES>
 cudaError_t launch_out(const Mx4View& a, const Mx4View& w, const Mx4Params& p, int dtype, int64_t max_tiles_m, cudaStream_t stream) {
+    if (p.out_codes)
+        return p.act == BIGMAC_ACT_GELU_ERF ? launch<BN, STAGES, OUT_MX4_GELU>(a, w, p, max_tiles_m, stream) : launch<BN, STAGES, OUT_MX4>(a, w, p, max_tiles_m, stream);
     if (dtype == BIGMAC_F32) return launch<BN, STAGES, OUT_F32>(a, w, p, max_tiles_m, stream);
     if (p.act == BIGMAC_ACT_IDENTITY) return launch<BN, STAGES, OUT_BF16>(a, w, p, max_tiles_m, stream);
     if (p.act == BIGMAC_ACT_GELU_ERF) return launch<BN, STAGES, OUT_BF16_GELU>(a, w, p, max_tiles_m, stream);
@@ -407,9 +436,11 @@ cudaError_t launch_out(const Mx4View& a, const Mx4View& w, const Mx4Params& p, i
 
 }  // namespace
 
-cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int dtype, void* c, int64_t ldc, int* status, cudaStream_t stream) {
+cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int dtype, void* c, int64_t ldc, const Mx4View* out, int* status,
+                              cudaStream_t stream) {
     if (a.rows == 0 || w.rows == 0) return cudaSuccess;
     Mx4Params p{};
+    if (out) { p.out_codes = out->codes; p.out_scales = out->scales; }
     p.C = c; p.ldc = ldc; p.sa = a.scales; p.sw = w.scales; p.offsets = a.offsets;
     p.M = a.rows; p.N = w.rows; p.K = a.K; p.E = a.E; p.capacity = a.capacity;
     p.act = act; p.status = status;

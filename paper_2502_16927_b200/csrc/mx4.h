@@ -53,6 +53,29 @@ __device__ __forceinline__ int mx4_find(const int32_t* table, int E, int v) {
     }
     return lo;
 }
+// Eight values to four bytes of codes.
+__device__ __forceinline__ uint32_t mx4_e2m1x8(const float* v) {
+    uint32_t out;
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t}"
+        : "=r"(out) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return out;
+}
+__device__ __forceinline__ float max_nan(float a, float b) { float d; asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b)); return d; }
+// The scale byte of a block whose largest magnitude is `top` (a NaN if it has one).
+__device__ __forceinline__ uint32_t mx4_scale_byte(float top) {
+    const uint32_t bits = __float_as_uint(top);
+    return bits < 0x7f800000u ? (uint32_t)max((int)(bits >> 23) - 2, 0) : 255u;
+}
+// The factor 2^(127 - s), twice, as a pair of fp32 numbers.
+__device__ __forceinline__ unsigned long long mx4_factor2(uint32_t s) {
+    const unsigned long long f = (unsigned long long)(254u - s) << 23;
+    return f | f << 32;
+}
 #endif
 
 struct Mx4View {                      // one matrix, or E stacked ones (weights), or the segments of E experts (offsets set)
@@ -65,6 +88,8 @@ struct Mx4View {                      // one matrix, or E stacked ones (weights)
 cudaError_t launch_mx4_quantize(const void* x, int dtype, int64_t ld, const int32_t* slot_of_row, int k, int x_rows, const Mx4View& out,
                                 cudaStream_t stream);
 cudaError_t launch_mx4_dequantize(const Mx4View& q, void* y, int dtype, int64_t ld, cudaStream_t stream);
-cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int dtype, void* c, int64_t ldc, int* status, cudaStream_t stream);
+// act(a w^T) to c (bf16 or fp32) or, with `out`, to a matrix in 4 bits with a's rows (c, dtype unused).
+cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int dtype, void* c, int64_t ldc, const Mx4View* out, int* status,
+                              cudaStream_t stream);
 
 }  // namespace bigmac

@@ -72,19 +72,6 @@ struct Chunks {
     }
 };
 
-// Eight values to four bytes of codes.
-__device__ __forceinline__ uint32_t e2m1x8(const float* v) {
-    uint32_t out;
-    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
-        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
-        "mov.b32 %0, {a, b, c, d};\n\t}"
-        : "=r"(out) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
-    return out;
-}
-
 // A block's 32 elements as they lie in memory; their largest magnitude (a NaN if there is one); the codes of their products with a power of two.
 template <typename T>
 struct Block {
@@ -135,9 +122,8 @@ struct Block {
             asm("mul.rn.f32x2 %0, %0, %1;" : "+l"(z) : "l"(factor2));
             asm("mov.b64 {%0, %1}, %2;" : "=f"(v[2 * i]), "=f"(v[2 * i + 1]) : "l"(z));
         }
-        return e2m1x8(v);
+        return mx4_e2m1x8(v);
     }
-    static __device__ __forceinline__ float max_nan(float a, float b) { float d; asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b)); return d; }
 };
 
 template <typename T>
@@ -167,17 +153,15 @@ __global__ void __launch_bounds__(kThreads, 5) mx4_quantize_kernel(const T* __re
             Block<T> v;
             if (mine && src >= 0) v.load(x + (int64_t)src * ld + b * 32, by32);
             else v.clear();
-            const uint32_t bits = __float_as_uint(v.top());             // of an infinity or a NaN: 0x7f800000 or more
-            const bool finite = bits < 0x7f800000u;
-            const uint32_t s = finite ? (uint32_t)max((int)(bits >> 23) - 2, 0) : 255u;
+            const uint32_t s = mx4_scale_byte(v.top());
             // four blocks' bytes to a word (zero behind the last block of the row)
             uint32_t word = mine ? s << (8 * (b & 3)) : 0u;
             word |= __shfl_xor_sync(kAll, word, 1);
             word |= __shfl_xor_sync(kAll, word, 2);
             if (mine) {
                 uint4 codes = make_uint4(0u, 0u, 0u, 0u);
-                if (finite) {
-                    const unsigned long long factor = (unsigned long long)(254u - s) << 23, factor2 = factor | factor << 32;
+                if (s != 255u) {
+                    const unsigned long long factor2 = mx4_factor2(s);
                     codes = make_uint4(v.codes(0, factor2), v.codes(1, factor2), v.codes(2, factor2), v.codes(3, factor2));
                 }
                 *(uint4*)(q.codes + (int64_t)row * (q.K / 2) + b * 16) = codes;

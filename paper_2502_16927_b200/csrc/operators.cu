@@ -171,7 +171,22 @@ int bigmac_mx4_matmul(const bigmac_mx4_t* a, const bigmac_mx4_t* w, int32_t act,
     if (!c) return BIGMAC_ERR_INVALID_ARG;
     int* status = status_word();
     if (!status) return BIGMAC_ERR_CUDA;
-    return launch_mx4_matmul(view_of(a), view_of(w), act, dtype, c, ldc, status, (cudaStream_t)stream) == cudaSuccess ? BIGMAC_OK : BIGMAC_ERR_CUDA;
+    return launch_mx4_matmul(view_of(a), view_of(w), act, dtype, c, ldc, nullptr, status, (cudaStream_t)stream) == cudaSuccess ? BIGMAC_OK : BIGMAC_ERR_CUDA;
+}
+
+int bigmac_mx4_matmul_mx4(const bigmac_mx4_t* a, const bigmac_mx4_t* w, int32_t act, const bigmac_mx4_t* out, void* stream) {
+    int s = check_mx4(a, false);
+    if (s == BIGMAC_OK) s = check_mx4(w, true);
+    if (s == BIGMAC_OK) s = check_mx4(out, false);
+    if (s != BIGMAC_OK) return s;
+    if (act < 0 || act > BIGMAC_ACT_IDENTITY || w->offsets || a->K != w->K || a->E != w->E || out->rows != a->rows || out->K != w->rows ||
+        out->E != a->E || out->offsets != a->offsets || out->codes == a->codes || out->scales == a->scales)
+        return BIGMAC_ERR_INVALID_ARG;
+    if (a->rows == 0) return BIGMAC_OK;
+    int* status = status_word();
+    if (!status) return BIGMAC_ERR_CUDA;
+    const Mx4View to = view_of(out);
+    return launch_mx4_matmul(view_of(a), view_of(w), act, 0, nullptr, 0, &to, status, (cudaStream_t)stream) == cudaSuccess ? BIGMAC_OK : BIGMAC_ERR_CUDA;
 }
 
 }  // extern "C"

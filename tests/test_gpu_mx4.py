@@ -230,6 +230,48 @@ def test_grouped_rows_in_no_segment_are_left(binding):
     assert bool((back[63:] == 2.0).all())
 
 
+@pytest.mark.parametrize("act", [0, 1, 2, 3])
+@pytest.mark.parametrize("E,rows,N,K", [(0, 1, 32, 64), (0, 300, 160, 256), (0, 1000, 1024, 128), (0, 2600, 4096, 64), (8, 700, 96, 96), (64, 512, 1024, 256)])
+def test_product_in_4_bits(binding, E, rows, N, K, act):
+    """The result's values are roundings of act(a w^T): a block's scale is that of its largest magnitude, a code off by half a step of its
+    place (or more where the fp32 value lies next to a border: then the neighbour's half step), magnitudes above 6 scales at 6."""
+    rng = _gen(rows + N + act)
+    x64 = np.round(rng.standard_normal((rows, K)) * 16) / 16
+    wc, wb, codes, scales = _weights(rng, (E,) if E else (), N, K)
+    offsets = _segments(rng, E, rows, "skewed") if E else np.array([0, rows])
+    off = torch.from_numpy(offsets.astype(np.int32)).cuda() if E else None
+    q = binding.mx4_matmul_mx4(binding.mx4_quantize(torch.from_numpy(x64).float().cuda(), offsets=off), binding.Mx4(codes, scales), act=act)
+    got = binding.mx4_dequantize(q, torch.float32).double().cpu().numpy()
+    a, w = ref.values(*ref.quantise(x64)), ref.values(wc, wb).reshape(-1, N, K)
+    for e in range(max(E, 1)):
+        seg = slice(offsets[e], offsets[e + 1])
+        if seg.start == seg.stop:
+            continue
+        z = a[seg] @ w[e].T
+        want = _act(z, act)
+        S = np.abs(a[seg]) @ np.abs(w[e]).T
+        err = 1.13 * (K / 64 + 2) * 2.0 ** -23 * S + (3.3e-5 if act == 1 else np.abs(z) * 2.0 ** -20)     # as for a product in bf16, without its rounding
+        blocks, slack = want.reshape(-1, N // 32, 32), err.reshape(-1, N // 32, 32)
+        top = np.abs(blocks).max(-1, keepdims=True)
+        ok = np.zeros(blocks.shape, dtype=bool)
+        for lean in (-1, 1):                                            # the largest magnitude as computed lies between these two
+            bound = np.maximum(top + lean * slack.max(-1, keepdims=True), 2.0 ** -125)
+            scale = 2.0 ** (np.floor(np.log2(bound)) - 2)
+            v = np.abs(blocks) / scale
+            step = np.where(v < 2, 0.5, np.where(v < 4, 1.0, 2.0))      # of the codes around v
+            near = np.where(v > 6, v - 6, step / 2) * scale             # above 6: down to 6
+            ok |= np.abs(got[seg].reshape(blocks.shape) - blocks) <= near * (1 + 1e-12) + slack
+        assert ok.all(), float((~ok).mean())
+    if E == 0 or rows > 128:                                            # what comes out is a matrix that the next product takes
+        w2c, w2b, c2, s2 = _weights(rng, (E,) if E else (), 64, N)
+        y = binding.mx4_matmul(q, binding.Mx4(c2, s2), dtype=torch.float32)
+        for e in range(max(E, 1)):
+            seg = slice(offsets[e], offsets[e + 1])
+            if seg.stop > seg.start:
+                _check_product(y[seg], got[seg], ref.values(w2c, w2b).reshape(-1, 64, N)[e], 3, torch.float32)
+    assert binding.operator_status() == 0
+
+
 def test_slots_that_name_no_row_give_zeros(binding):
     x = torch.ones(3, 32, dtype=torch.float32, device="cuda")
     slot = torch.tensor([0, -1, 5, 6, 2 ** 31 - 1], dtype=torch.int32, device="cuda")

@@ -77,6 +77,16 @@ def test_mx4_dequantize_and_matmul_refusals(lib):
                dict(w=_mx4(rows=8, E=2)), dict(a=_mx4(E=2, offsets=HERE)), dict(a=_mx4(E=2, offsets=HERE), w=_mx4(rows=8, E=3)),
                dict(a=_mx4(E=2, offsets=HERE), w=_mx4(rows=8, E=2, offsets=HERE))):
         assert product(**kw) == -1, kw
+    def product4(a=None, w=None, act=3, out=None):
+        return lib.bigmac_mx4_matmul_mx4(C.byref(a or _mx4()), C.byref(w or _mx4(rows=32)), act, C.byref(out or _mx4(2 * HERE, 2 * HERE, K=32)), None)
+
+    assert lib.bigmac_mx4_matmul_mx4(None, C.byref(_mx4()), 3, C.byref(_mx4()), None) == -1
+    for kw in (dict(act=4), dict(a=_mx4(K=32)), dict(w=_mx4(rows=64)), dict(out=_mx4(2 * HERE, 2 * HERE, rows=5, K=32)), dict(out=_mx4(K=32)),
+               dict(out=_mx4(2 * HERE, 2 * HERE, K=32, E=1, offsets=HERE)), dict(out=_mx4(2 * HERE, 2 * HERE, K=64)),
+               dict(a=_mx4(E=1, offsets=HERE), w=_mx4(rows=32, E=1), out=_mx4(2 * HERE, 2 * HERE, K=32, E=1, offsets=2 * HERE))):
+        assert product4(**kw) == -1, kw
+    assert product4(out=_mx4(2 * HERE, 2 * HERE, K=48), w=_mx4(rows=48)) == -2
+    assert product4(a=_mx4(rows=0), out=_mx4(2 * HERE, 2 * HERE, rows=0, K=32)) == 0
     # nothing to do is no error and touches nothing
     assert product(a=_mx4(rows=0)) == 0 and product(w=_mx4(rows=0)) == 0
 
