@@ -388,6 +388,15 @@ int bigmac_mx4_matmul(const bigmac_mx4_t *a, const bigmac_mx4_t *w, int32_t act,
  * has a's rows, K = w->rows (a multiple of 32) and, grouped, a's E and the same offsets: the input of a next product. */
 int bigmac_mx4_matmul_mx4(const bigmac_mx4_t *a, const bigmac_mx4_t *w, int32_t act, const bigmac_mx4_t *out, void *stream);
 
+/* The inference forward of a layer whose experts' weights are in 4 bits: w1 the E matrices [h, r], w2 the E matrices [r, h]
+ * (W->w1 and W->w2 are not read); W'_down, W'_up, the gate and everything outside the experts as in bigmac_forward.  The rows of x'
+ * and the hidden activations are quantised on the way: u = Q(sigma(Q(x') Q(W1_e)^T)) Q(W2_e)^T.  BF16 handles on
+ * the tensor cores, without expert biases (UNSUPPORTED otherwise).  scratch: bigmac_mx4_workspace_bytes. */
+int bigmac_mx4_workspace_bytes(const bigmac_layer_t *L, int32_t T, size_t *scratch_bytes);
+int bigmac_forward_mx4(bigmac_layer_t *L, const void *x, int32_t T, const bigmac_weights_t *W, const bigmac_mx4_t *w1,
+                       const bigmac_mx4_t *w2, void *y, bigmac_routing_t *routing_out, void *scratch, size_t scratch_bytes,
+                       void *stream);
+
 /* bigmac_route for callers that cannot provide scratch memory.  (The paper has no counterpart: this is
  * a deployment variant of the routing step, not part of the method.)
  *

@@ -126,6 +126,10 @@ def lib() -> C.CDLL:
         L.bigmac_mx4_matmul.argtypes = [Q, Q, i32, i32, vp, i64, vp]
         L.bigmac_mx4_matmul_mx4.argtypes = [Q, Q, i32, Q, vp]
         L.bigmac_mx4_matmul_mx4.restype = C.c_int
+        L.bigmac_mx4_workspace_bytes.argtypes = [vp, i32, C.POINTER(sz)]
+        L.bigmac_mx4_workspace_bytes.restype = C.c_int
+        L.bigmac_forward_mx4.argtypes = [vp, vp, i32, C.POINTER(bigmac_weights_t), Q, Q, vp, C.POINTER(bigmac_routing_t), vp, sz, vp]
+        L.bigmac_forward_mx4.restype = C.c_int
         L.bigmac_residual_norm_forward.argtypes = [vp, i32, vp]
         L.bigmac_residual_norm_scratch_bytes.argtypes = [vp, i32, C.POINTER(sz)]
         L.bigmac_residual_norm_backward.argtypes = [vp, i32, C.c_int, vp, sz, vp]
@@ -455,13 +459,14 @@ def _joint(x, shape, dtype, y, gate, gate_kind, post, pre, residual_scale, here)
 
 def residual_norm_forward(x: torch.Tensor, y: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, post: Optional[Norm] = None,
                           pre: Optional[Norm] = None, residual_scale: float = 1.0, training: bool = False, gate_kind: Optional[int] = None,
-                          r: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None):
+                          r: Optional[torch.Tensor] = None, n: Optional[torch.Tensor] = None, want_r: bool = True):
     """r = residual_scale x + gate N_post(y) and n = N_pre(r) (bigmac_residual_norm_forward): (r, n, stats), n None without `pre`, stats (for
-    the backward) None unless `training`.  gate: [T] or [d] fp32, or [T, d].  r and n may be given, in place too (r is x, n is y)."""
+    the backward) None unless `training`.  gate: [T] or [d] fp32, or [T, d].  r and n may be given, in place too (r is x, n is y); r is
+    neither written nor returned without want_r."""
     here, shape, dtype = _here(), x.shape, x.dtype
     members = _joint(x, shape, dtype, y, gate, gate_kind, post, pre, residual_scale, here)
     T, d = shape
-    if r is None:
+    if r is None and want_r:
         r = torch.empty_like(x)
         r_at, r_ld = r.data_ptr(), d
     else:
@@ -638,6 +643,26 @@ def mx4_matmul_mx4(a: Mx4, w: Mx4, act: int = 3) -> Mx4:
     return Mx4(codes, scales, a.offsets, a.rows)
 
 
+def mx4_quantize_weights(w: torch.Tensor) -> Mx4:
+    """The stacked weights [E, N, K] of E experts, laid out once."""
+    if w.dim() != 3:
+        raise ValueError("w: [E, N, K]")
+    parts = [mx4_quantize(one) for one in w]
+    return Mx4(torch.stack([q.codes for q in parts]), torch.stack([q.scales for q in parts]))
+
+
+def bigmac_mx4_workspace_bytes(handle, T: int) -> int:
+    n = C.c_size_t()
+    _check(lib().bigmac_mx4_workspace_bytes(handle, T, C.byref(n)), "bigmac_mx4_workspace_bytes")
+    return n.value
+
+
+def bigmac_forward_mx4(handle, x, T, W, w1: Mx4, w2: Mx4, y, routing, scratch) -> None:
+    here = _here()
+    _check(lib().bigmac_forward_mx4(handle, _ptr(x), T, C.byref(_weights(W)), C.byref(_mx4(w1, here)), C.byref(_mx4(w2, here)), _ptr(y), _routing(routing),
+                                    _ptr(scratch), scratch.numel() * scratch.element_size(), _stream()), "bigmac_forward_mx4")
+
+
 # ---- a small convenience wrapper: owns the handle and the workspaces ------------------------------------
 
 class Layer:
@@ -700,7 +725,30 @@ class Layer:
         bigmac_route(self.handle, x, T, W, R, self._scratch)
         return R
 
+    def _forward_mx4(self, x, W, y, want_routing):
+        """The inference forward with experts in 4 bits."""
+        T = x.shape[0]
+        need = self._need.get((T, "mx4"))
+        if need is None:
+            if len(self._need) >= 4096:
+                self._need.clear()
+            need = self._need[T, "mx4"] = bigmac_mx4_workspace_bytes(self.handle, T)
+        if self._scratch is None or self._scratch.numel() < need:
+            self._scratch = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
+        if y is None:
+            y = torch.empty_like(x)
+        R = self.empty_routing(T) if want_routing else None
+        shared = {name: t for name, t in W.items() if name not in ("w1", "w2")}
+        bigmac_forward_mx4(self.handle, x, T, shared, W["w1"], W["w2"], y, R, self._scratch)
+        self._T = None
+        return (y, R) if want_routing else y
+
     def forward(self, x, W, y=None, training=False, want_routing=False):
+        """W: the weights by name; w1 and w2 as `Mx4` (mx4_quantize_weights) run the experts in 4 bits (inference only)."""
+        if isinstance(W.get("w1"), Mx4) or isinstance(W.get("w2"), Mx4):
+            if training or not (isinstance(W["w1"], Mx4) and isinstance(W["w2"], Mx4)):
+                raise ValueError("experts in 4 bits: both w1 and w2, inference only")
+            return self._forward_mx4(x, W, y, want_routing)
         T = x.shape[0]
         self._workspaces(T, training)
         if y is None:
@@ -721,3 +769,35 @@ class Layer:
 
     def status(self) -> int:
         return bigmac_device_status(self.handle)
+
+
+class Block:
+    """The layer as a residual block: out = residual_scale x + gate N_post(layer(N_pre(x))), forward and backward, with the two joints of
+    residual_norm_forward around it.  pre, post: `Norm`s (post may be None); gate: a vector of parameters [d], or None."""
+
+    def __init__(self, layer: Layer, pre: Norm, post: Optional[Norm] = None, gate: Optional[torch.Tensor] = None, residual_scale: float = 1.0):
+        self.layer, self.pre, self.post, self.gate, self.residual_scale = layer, pre, post, gate, residual_scale
+        self._gate_kind = None if gate is None else BIGMAC_GATE_CHANNEL
+        self._kept = None
+
+    def forward(self, x, W, training=False, want_routing=False):
+        _, n, before = residual_norm_forward(x, pre=self.pre, training=training, want_r=False)
+        y = self.layer.forward(n, W, training=training, want_routing=want_routing)
+        y, R = y if want_routing else (y, None)
+        out, _, after = residual_norm_forward(x, y, self.gate, self.post, residual_scale=self.residual_scale, training=training, gate_kind=self._gate_kind)
+        self._kept = (x, n, y, before, after) if training else None
+        return (out, R) if want_routing else out
+
+    def backward(self, dout, W, G, accumulate=False):
+        """dx; G: the layer's gradient buffers and, of the block's own parameters, any of dw_pre, db_pre, dw_post, db_post (fp32 [d]) and
+        dgate."""
+        if self._kept is None:
+            raise RuntimeError("backward needs a training forward first")
+        x, n, y, before, after = self._kept
+        own = {name: G[name] for name in ("dw_post", "db_post", "dgate") if name in G}
+        dx, dy, _ = residual_norm_backward(x, y, self.gate, self.post, None, dout, None, after, own, self.residual_scale, accumulate, self._gate_kind)
+        dn = self.layer.backward(n, dy, W, G, accumulate=accumulate)
+        # the gradient through the norm joins the residual's
+        own = {name: G[name] for name in ("dw_pre", "db_pre") if name in G}
+        dx, _, _ = residual_norm_backward(x, None, None, None, self.pre, dx, dn, before, own, accumulate=accumulate)
+        return dx

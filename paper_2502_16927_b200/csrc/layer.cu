@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "layer_common.h"
+#include "mx4.h"
 #include "place_pool.h"
 #include "switches.h"
 
@@ -229,6 +230,41 @@ size_t saved_bytes_of(const Dims& m) {
     return cv.total();
 }
 
+
+// Intermediates of an inference forward with 4-bit experts: x', the rows of x' and the hidden activations in 4 bits, both grouped by
+// expert; u by the exported row numbers.
+struct Mx4Experts {
+    Mx4View w1, w2;      // [E, h, r], [E, r, h]
+    Mx4View xg, a;
+};
+void carve_mx4(Carver& cv, const Dims& m, Buffers& b, Mx4Experts& f) {
+    carve_route_scratch(cv, m, b);
+    carve_descend_split(cv, m, b);
+    b.tb.topk_idx = cv.take<int32_t>(m.N);
+    b.tb.topk_w = cv.take<float>(m.N);
+    b.tb.counts = cv.take<int32_t>(m.E);
+    b.tb.offsets = cv.take<int32_t>(m.E + 1);
+    b.tb.poffsets = cv.take<int32_t>(m.E + 1);
+    b.tb.row_of_slot = cv.take<int32_t>(m.N);
+    b.tb.slot_of_row = cv.take<int32_t>(m.N);
+    b.tb.prow_of_slot = cv.take<int32_t>(m.N);
+    b.tb.slot_of_prow = cv.take<int32_t>(m.P);
+    b.tb.tile_expert = cv.take<int32_t>(m.P / kPad);
+    b.tb.n_tiles = cv.take<int32_t>(1);
+    b.tb.counts_chosen = cv.take<int32_t>(m.E);
+    b.aux_loss = cv.take<float>(1);
+    b.x_lo = m.cdac ? nullptr : cv.take_bytes((size_t)m.T * m.r * 2);
+    b.u = cv.take_bytes((size_t)m.N * m.r * 2);
+    b.y_lo = m.cdac ? nullptr : cv.take_bytes((size_t)m.T * m.r * 2);
+    const int64_t rows = mx4_padded_rows(m.N, m.E);
+    auto grouped = [&](int K) {
+        uint8_t* codes = (uint8_t*)cv.take_bytes((size_t)rows * (K / 2));
+        uint8_t* scales = (uint8_t*)cv.take_bytes((size_t)(rows / kMx4Tile) * mx4_ktiles(K) * 512);
+        return Mx4View{codes, scales, (int)m.N, K, m.E, nullptr, rows};
+    };
+    f.xg = grouped(m.r);
+    f.a = grouped(m.h);
+}
 
 int check_weights(const bigmac_layer* L, const bigmac_weights_t* W) {
     if (!W || !W->w_gate || !W->w1 || !W->w2) return BIGMAC_ERR_INVALID_ARG;
@@ -634,8 +670,49 @@ int bigmac_route(bigmac_layer_t* L, const void* x, int32_t T, const bigmac_weigh
     return run_routing(L, m, x, W, b, b.a, out, st);
 }
 
+// `four` (nullable): inference with the experts' weights in 4 bits.
+static int forward_launches(bigmac_layer_t* L, const void* x, int32_t T, const bigmac_weights_t* W, Mx4Experts* four, void* y,
+                            bigmac_routing_t* routing_out, void* saved, void* scratch, size_t scratch_bytes, void* stream);
+
 int bigmac_forward(bigmac_layer_t* L, const void* x, int32_t T, const bigmac_weights_t* W, void* y,
                    bigmac_routing_t* routing_out, void* saved, void* scratch, size_t scratch_bytes, void* stream) {
+    return forward_launches(L, x, T, W, nullptr, y, routing_out, saved, scratch, scratch_bytes, stream);
+}
+
+static int mx4_experts_supported(const bigmac_layer* L) {
+    return L->cfg.dtype == BIGMAC_BF16 && L->use_tc && !(L->cfg.flags & BIGMAC_FLAG_EXPERT_BIAS);
+}
+
+int bigmac_mx4_workspace_bytes(const bigmac_layer_t* L, int32_t T, size_t* scratch_bytes) {
+    if (!L || !scratch_bytes || T < 0 || T > L->cfg.max_tokens) return BIGMAC_ERR_INVALID_ARG;
+    if (!mx4_experts_supported(L)) return BIGMAC_ERR_UNSUPPORTED;
+    Carver cv(nullptr);
+    Buffers b{};
+    Mx4Experts f{};
+    carve_mx4(cv, dims_of(L, T), b, f);
+    *scratch_bytes = cv.total();
+    return BIGMAC_OK;
+}
+
+int bigmac_forward_mx4(bigmac_layer_t* L, const void* x, int32_t T, const bigmac_weights_t* W, const bigmac_mx4_t* w1, const bigmac_mx4_t* w2, void* y,
+                       bigmac_routing_t* routing_out, void* scratch, size_t scratch_bytes, void* stream) {
+    BIGMAC_TRY(check_call(L, T));
+    if (!mx4_experts_supported(L)) return BIGMAC_ERR_UNSUPPORTED;
+    const bigmac_config_t& c = L->cfg;
+    auto fits = [&](const bigmac_mx4_t* w, int rows, int K) {
+        return w && w->codes && w->scales && aligned(w->codes, 16) && aligned(w->scales, 16) && w->rows == rows && w->K == K && w->E == c.E && !w->offsets;
+    };
+    if (!W || !fits(w1, c.h, c.r) || !fits(w2, c.r, c.h)) return BIGMAC_ERR_INVALID_ARG;
+    bigmac_weights_t shared = *W;
+    shared.w1 = w1->codes; shared.w2 = w2->codes;                 // present, so that the others are checked; not read as weights
+    Mx4Experts four{};
+    four.w1 = Mx4View{(uint8_t*)w1->codes, (uint8_t*)w1->scales, c.h, c.r, c.E, nullptr, c.h};
+    four.w2 = Mx4View{(uint8_t*)w2->codes, (uint8_t*)w2->scales, c.r, c.h, c.E, nullptr, c.r};
+    return forward_launches(L, x, T, &shared, &four, y, routing_out, nullptr, scratch, scratch_bytes, stream);
+}
+
+static int forward_launches(bigmac_layer_t* L, const void* x, int32_t T, const bigmac_weights_t* W, Mx4Experts* four, void* y,
+                            bigmac_routing_t* routing_out, void* saved, void* scratch, size_t scratch_bytes, void* stream) {
     BIGMAC_TRY(check_call(L, T));
     BIGMAC_TRY(check_weights(L, W));
     if (T == 0) return BIGMAC_OK;
@@ -644,24 +721,31 @@ int bigmac_forward(bigmac_layer_t* L, const void* x, int32_t T, const bigmac_wei
         return BIGMAC_ERR_INVALID_ARG;
     const bool training = saved != nullptr;
     const Dims m = dims_of(L, T);
-    if (scratch_bytes < forward_scratch_bytes(m, training)) return BIGMAC_ERR_WORKSPACE;
     Buffers b{};
-    Carver cs(scratch);
-    carve_route_scratch(cs, m, b);
-    carve_descend_split(cs, m, b);
-    if (training) {
-        Carver cv(saved);
-        carve_saved(cv, m, b, true);
-        if (b.logits_saved) b.logits = b.logits_saved;        // the backward of the load-balancing loss reads them
-    } else {
-        carve_saved(cs, m, b, false);
+    if (four) {
+        Carver cs(scratch);
+        carve_mx4(cs, m, b, *four);
+        if (scratch_bytes < cs.total()) return BIGMAC_ERR_WORKSPACE;
         alias_routing(b, routing_out);
+    } else {
+        if (scratch_bytes < forward_scratch_bytes(m, training)) return BIGMAC_ERR_WORKSPACE;
+        Carver cs(scratch);
+        carve_route_scratch(cs, m, b);
+        carve_descend_split(cs, m, b);
+        if (training) {
+            Carver cv(saved);
+            carve_saved(cv, m, b, true);
+            if (b.logits_saved) b.logits = b.logits_saved;        // the backward of the load-balancing loss reads them
+        } else {
+            carve_saved(cs, m, b, false);
+            alias_routing(b, routing_out);
+        }
     }
     cudaStream_t st = (cudaStream_t)stream;
     const bigmac_config_t& c = L->cfg;
 
     // A few tokens, inference: the whole forward in one cooperative kernel (weight streaming, no tensor cores)
-    if (!training && !m.cdac && !m.gate_low && !m.bias && m.cap == kNoCapacity && m.aux == 0 && sigma_as_bytes(L) && L->decode_words &&
+    if (!training && !four && !m.cdac && !m.gate_low && !m.bias && m.cap == kNoCapacity && m.aux == 0 && sigma_as_bytes(L) && L->decode_words &&
         decode_forward_supported(m.T, m.d, m.r, m.h, m.E, m.k, m.dtype, gemm_tc_sm_count())) {
         {
             Stage s(L, S_DECODE, st);
@@ -679,7 +763,7 @@ int bigmac_forward(bigmac_layer_t* L, const void* x, int32_t T, const bigmac_wei
     const int bn_desc = (m.r + m.E) >= 256 ? 256 : 128;
     const bool fuse_gate = !m.cdac && !m.gate_low && c.dtype == BIGMAC_BF16 && L->use_tc && L->tc_mask == ~0u && m.r % bn_desc == 0;
     if (m.cdac) b.x_lo = const_cast<void*>(x);                                    // Eq. 3: experts read the token itself
-    const bool gather_dispatch = dispatch_is_fused(L, m, training);
+    const bool gather_dispatch = !four && dispatch_is_fused(L, m, training);
     RouteSource src{b.logits, m.E, 1, 0, nullptr};
     RouteMove mv{};
     if (fuse_gate) {
@@ -692,7 +776,7 @@ int bigmac_forward(bigmac_layer_t* L, const void* x, int32_t T, const bigmac_wei
         // 20 us.  Up to 80 MB: beside the rest they fit in L2 (126 MB).  At 3001 tokens, 375 rows an expert, the hint only
         // slowed the descend launch (13 -> 19 us).
         const size_t expert_bytes = (size_t)m.E * m.h * m.r * esize(m.dtype);
-        if (!training && uses_fused_mlp(L, m) && m.N >= 2 * (int64_t)m.E && m.N <= 128 * (int64_t)m.E && 2 * expert_bytes <= ((size_t)80 << 20)) {
+        if (!training && !four && uses_fused_mlp(L, m) && m.N >= 2 * (int64_t)m.E && m.N <= 128 * (int64_t)m.E && 2 * expert_bytes <= ((size_t)80 << 20)) {
             g.prefetch[0] = W->w1; g.prefetch[1] = W->w2; g.prefetch_bytes = expert_bytes;
         }
         if (b.descend_ws) {                                   // few tokens: contraction in parts, added by the routing kernels
@@ -701,7 +785,7 @@ int bigmac_forward(bigmac_layer_t* L, const void* x, int32_t T, const bigmac_wei
             g.split_k = parts; g.out_f32 = true;
             g.C = b.descend_ws; g.ldc = ld; g.C2 = b.descend_ws + m.r; g.ldc2 = ld;
             BIGMAC_TRY(gemm(L, G_DESCEND, g, st));
-            if (route_fused_supported(m.E, m.k) && !gather_dispatch) {
+            if (route_fused_supported(m.E, m.k) && !gather_dispatch && !four) {
                 src = RouteSource{b.descend_ws + m.r, ld, parts, part_stride, m.aux > 0 ? b.logits : nullptr};
                 mv.partial = b.descend_ws; mv.ld = ld; mv.parts = parts; mv.part_stride = part_stride;
             } else {
@@ -725,15 +809,21 @@ int bigmac_forward(bigmac_layer_t* L, const void* x, int32_t T, const bigmac_wei
     // F2, F3 and F5 (dispatch at width r) - unless the dispatch is fused into its consumers: expert GEMM1's producer warp
     // then gathers the rows of x' itself (slot_of_prow names the token of every grouped row, -1 the zero padding rows) and
     // the grouped copy xg is never written.
-    if (!gather_dispatch) {
+    if (!gather_dispatch && !four) {
         mv.src = b.x_lo; mv.grouped = b.xg; mv.row_bytes = m.r * (int)esize(m.dtype); mv.zero_padding = training;
     }
     BIGMAC_TRY(route_from_logits(L, m, W, b, src, mv, aux_word_to_zero(m, routing_out), routing_out, st));
     // Inference: F6 + F7 in one kernel, the hidden activations stay on the SM (uses_fused_mlp has the rule).
-    const bool in_pairs = !gather_dispatch && uses_ffn(L, m, training);
-    const bool mlp_fused = !training && !in_pairs && uses_fused_mlp(L, m);
+    const bool in_pairs = !four && !gather_dispatch && uses_ffn(L, m, training);
+    const bool mlp_fused = !four && !training && !in_pairs && uses_fused_mlp(L, m);
     const MlpSlicing slicing = fused_mlp_slicing(m.r, m.h, m.N, m.P);
-    if (mlp_fused) {
+    if (four) {
+        // the dispatch while the rows are quantised, F6 with the hidden activations straight to 4 bits, F7, F8 by the exported row numbers
+        four->xg.offsets = four->a.offsets = b.tb.offsets;
+        { Stage s(L, S_MX4_QUANTIZE, st); BIGMAC_CUDA(launch_mx4_quantize(b.x_lo, m.dtype, m.r, b.tb.slot_of_row, m.k, m.T, four->xg, st)); }
+        { Stage s(L, S_MX4_EXPERTS, st); BIGMAC_CUDA(launch_mx4_matmul(four->xg, four->w1, c.act, 0, nullptr, 0, &four->a, L->status, st)); }
+        { Stage s(L, S_MX4_EXPERTS, st); BIGMAC_CUDA(launch_mx4_matmul(four->a, four->w2, BIGMAC_ACT_IDENTITY, BIGMAC_BF16, b.u, m.r, nullptr, L->status, st)); }
+    } else if (mlp_fused) {
         Stage s(L, S_FUSED_MLP, st);
         BIGMAC_CUDA(launch_fused_mlp(b.xg, W->w1, W->w2, b.a, m.P, m.N, slicing, m.r, m.h, m.E, c.act, b.tb, L->status, st));
     } else if (uses_ffn_simt(L, m)) {
@@ -766,7 +856,7 @@ int bigmac_forward(bigmac_layer_t* L, const void* x, int32_t T, const bigmac_wei
     if (mlp_fused) {                                                              // F8
         Stage s(L, S_COMBINE, st);
         BIGMAC_CUDA(launch_combine_parts(b.a, slicing, b.tb.n_tiles, b.y_lo, b.tb.topk_w, b.tb.prow_of_slot, m.T, m.k, m.r, st, m.cap != kNoCapacity));
-    } else { Stage s(L, S_COMBINE, st); BIGMAC_CUDA(launch_combine(b.u, b.y_lo, b.tb.topk_w, b.tb.prow_of_slot, m.T, m.k, m.r, m.dtype, st, 0, m.cap != kNoCapacity)); }  // F8
+    } else { Stage s(L, S_COMBINE, st); BIGMAC_CUDA(launch_combine(b.u, b.y_lo, b.tb.topk_w, four ? b.tb.row_of_slot : b.tb.prow_of_slot, m.T, m.k, m.r, m.dtype, st, 0, m.cap != kNoCapacity)); }  // F8
     if (!m.cdac) {                                                                // F9 ascend: y = y' W'_up
         GemmArgs g;
         g.A = b.y_lo; g.lda = m.r; g.B = W->w_up; g.ldb = m.r; g.C = y; g.ldc = m.d;

@@ -162,3 +162,9 @@ def test_residual_norm_refusals(lib):
     assert lib.bigmac_residual_norm_scratch_bytes(_joint(**back, db_pre=HERE), 4, C.byref(need)) == 0 and need.value >= 4 * 64 * 4
     assert lib.bigmac_residual_norm_scratch_bytes(_joint(**back, db_pre=HERE), 0, C.byref(need)) == 0 and need.value == 0
     assert lib.bigmac_residual_norm_scratch_bytes(None, 4, C.byref(need)) == -1
+
+
+def test_forward_with_4_bit_experts_refuses_null_handles(lib):
+    size = C.c_size_t()
+    assert lib.bigmac_forward_mx4(None, None, 0, None, None, None, None, None, None, 0, None) == -1
+    assert lib.bigmac_mx4_workspace_bytes(None, 1, C.byref(size)) == -1
