@@ -12,134 +12,13 @@
 // fills and the other set stores: with all sixteen on one accumulator every latency of a tile (barrier, tensor memory, stores) was waited out
 // by all (131072 rows, r 256 -> h 1024: 142 us).  bf16 rows leave through shared memory and TMA, 128 bytes a row; 32-byte stores of the
 // lanes' own rows alone took 1350 cycles a tile.
-#include "tc_common.cuh"
-#include "mx4.h"
+#include "gemm_mx4.cuh"
 
 namespace bigmac {
 
-using namespace tc;
+using namespace mx4;
 
 namespace {
-
-constexpr int kSliceK = 256;                               // columns of a stage: one 128-byte row of codes
-constexpr uint32_t kABytes = 128 * 128;
-constexpr uint32_t kSfTile = 512;
-constexpr int kEpi = 16;                                   // epilogue warps, two sets with two to a lane quadrant
-constexpr int kThreadsMx4 = (2 + kEpi) * 32;
-
-struct Mx4Params {
-    void* C;
-    int64_t ldc;
-    const uint8_t *sa, *sw;                                // scale bytes
-    uint8_t *out_codes, *out_scales;                       // OUT_MX4: the result's
-    const int32_t* offsets;                                // grouped: the caller's table
-    int M, N, K, E;
-    int64_t capacity;                                      // rows that A has room for (grouped)
-    int act, tma_store;
-    int box_rows;                                          // of A's codes: a tile with few rows loads few
-    int* status;
-};
-
-__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
-                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
-}
-// 512 bytes of scales, 32 rows of 16 bytes, to four columns of tensor memory in all four lane quadrants.
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
-}
-// Without swizzle: groups of 8 rows of 16 bytes, 128 bytes apart.
-__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
-    return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
-}
-__device__ __forceinline__ void umma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %6, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
-        : "memory");
-}
-// Instruction descriptor: e2m1 x e2m1, scales ue8m0, M 128, N bn; `half`: which two of a column's four scale bytes.
-__host__ __device__ constexpr uint32_t instr_desc_mx4(int bn, int half) {
-    return ((uint32_t)(2 * half) << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(bn >> 3) << 17) | (1u << 23) | ((uint32_t)(128 >> 4) << 24) |
-           ((uint32_t)(2 * half) << 29);
-}
-
-// GELU of 32 accumulators for an output in bf16: z Phi(z), Phi(z) = sat(1/2 + z P(z^2)).  P is the minimax fit in the error of z Phi(z) on
-// |z| <= 4.5 (reweighted least squares on Chebyshev nodes), of even degree with a positive leading coefficient, so that behind 4.5 the
-// saturating multiply-add holds Phi at 0 or 1 without a look at the argument.  z Phi(z) is off by less than 3e-6 up to 4.5 and by less
-// than 3.3e-5 everywhere (at -4.5, where it is -1.5e-5 itself): a bf16 step of 1/2 is 4e-3.  Seven instructions an element; a form that
-// keeps the relative precision of the negative tail (a polynomial times an exponential) took twelve and, at 131072 rows of r 256, h 1024,
-// 96 us, erff 142.
-__device__ __forceinline__ void gelu_chunk(float* v) {
-    constexpr float kC[11] = {0.3989286422729492f, -0.06644835323095322f, 0.009928264655172825f, -0.0011627154890447855f, 0.00010752371599664912f, -7.800386811140925e-06f,
-                              4.3196823185098765e-07f, -1.7442022937075308e-08f, 4.790651764174925e-10f, -7.938010491981284e-12f, 5.954283154854453e-14f};
-    constexpr int kG = 8;                                  // pairs side by side, so that no multiply-add waits for the one before
-#pragma unroll
-    for (int g = 0; g < 16; g += kG) {
-        f32x2_t w[kG], P[kG];
-#pragma unroll
-        for (int i = 0; i < kG; ++i) {
-            const f32x2_t z = pk2(v[2 * (g + i)], v[2 * (g + i) + 1]);
-            w[i] = mul2(z, z);
-            P[i] = fma2(pk2(kC[10], kC[10]), w[i], pk2(kC[9], kC[9]));
-        }
-#pragma unroll
-        for (int k = 8; k >= 0; --k)
-#pragma unroll
-            for (int i = 0; i < kG; ++i) P[i] = fma2(P[i], w[i], pk2(kC[k], kC[k]));
-#pragma unroll
-        for (int i = 0; i < kG; ++i) {
-            float &z0 = v[2 * (g + i)], &z1 = v[2 * (g + i) + 1], p0, p1;
-            upk2(P[i], p0, p1);
-            upk2(mul2(pk2(z0, z1), pk2(fma_sat(z0, p0, 0.5f), fma_sat(z1, p1, 0.5f))), z0, z1);
-        }
-    }
-}
-
-// The tiles of a walker: t, t + step, ...  All columns of a row tile follow each other (its codes stay in L2).
-struct Mx4Tables {                                         // grouped: shared memory
-    const int32_t *prefix, *first, *end;                   // row tiles before expert e [E + 1]; its rows in the caller's order
-};
-struct Mx4Walk {
-    int mt, nt, e, step_m, step_n, tiles_n;
-    __device__ __forceinline__ void init(int t, int step, int n) {
-        tiles_n = n;
-        mt = t / n; nt = t - mt * n;
-        step_m = step / n; step_n = step - step_m * n;
-        e = 0;
-    }
-    __device__ __forceinline__ void next() {
-        mt += step_m; nt += step_n;
-        if (nt >= tiles_n) { nt -= tiles_n; ++mt; }
-    }
-    // The expert of row tile mt, which never falls from tile to tile.
-    __device__ __forceinline__ int expert(const Mx4Tables& tb, int E) {
-        while (e + 1 < E && tb.prefix[e + 1] <= mt) ++e;
-        return e;
-    }
-};
-struct Mx4Rows {
-    int expert, c_row, rows;                               // first row in C, rows of this tile that exist
-};
-__device__ __forceinline__ Mx4Rows mx4_rows(const Mx4Params& p, const Mx4Tables& tb, Mx4Walk& w) {
-    if (!p.offsets) return {0, w.mt * kMx4Tile, min(kMx4Tile, p.M - w.mt * kMx4Tile)};
-    const int e = w.expert(tb, p.E), c = tb.first[e] + (w.mt - tb.prefix[e]) * kMx4Tile;
-    return {e, c, min(kMx4Tile, tb.end[e] - c)};
-}
-
-// 32 columns of a row, packed, to the warp's box of 32 rows by COLS columns, laid out for a TMA store with the swizzle of its row's width.
-template <int COLS>
-__device__ __forceinline__ void stage_row(uint8_t* box, int lane, int chunk, const uint32_t* w) {
-    if (COLS == 64) {
-        uint8_t* row = box + lane * 128;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) st_shared_16B(row + (((chunk * 4 + j) ^ (lane & 7)) << 4), w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
-    } else {
-        stage_row_bf16(box, lane, w);
-    }
-}
 
 template <int BN, int STAGES>
 struct Mx4Smem {
@@ -153,30 +32,6 @@ struct Mx4Smem {
     static constexpr uint32_t kBars = (2 * STAGES + 4) * 8 + 16;
     static constexpr size_t bytes(int E) { return 1024 + STAGES * kStage + kEpi * kBox + kBars + (size_t)(3 * E + 1) * 4; }
 };
-
-// 32 columns of a row are a block of the result in 4 bits: its scale and codes from the fp32 numbers, without a rounding between.
-__device__ __forceinline__ void store_block(const Mx4Params& p, float* v, int row, int block) {
-    float top = 0.0f;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) top = max_nan(top, fabsf(v[i]));
-    const uint32_t s = mx4_scale_byte(top);
-    uint32_t c[4] = {0u, 0u, 0u, 0u};
-    if (s != 255u) {
-        const f32x2_t factor = mx4_factor2(s);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) upk2(mul2(pk2(v[2 * i], v[2 * i + 1]), factor), v[2 * i], v[2 * i + 1]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = mx4_e2m1x8(v + 8 * i);
-    }
-    *(uint4*)(p.out_codes + (int64_t)row * (p.N / 2) + block * 16) = make_uint4(c[0], c[1], c[2], c[3]);
-    uint8_t* at = p.out_scales + mx4_scale_at(row, block, mx4_ktiles(p.N));
-    *at = (uint8_t)s;
-    if (block + 1 == p.N / 32)
-        for (int b = block + 1; b & 3; ++b) *++at = 0;                   // behind the last block of the row
-}
-
-// What the epilogue does is fixed at compile time: with every way in one kernel its warps waited for instructions.
-enum { OUT_BF16 = 0, OUT_BF16_GELU, OUT_BF16_ACT, OUT_F32, OUT_MX4_GELU, OUT_MX4 };
 
 template <int BN, int STAGES, int OUT>
 __global__ void __launch_bounds__(kThreadsMx4, 1)
@@ -304,88 +159,31 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         // ------------------------------------------------------------------ epilogue: set `acc` drains accumulator `acc`
         const int quad = warp & 3, half = ((warp - 2) >> 2) & 1;
         const uint32_t acc = (uint32_t)(warp - 2) >> 3;
-        constexpr int kChunks = S::kCols / 32;
-        uint8_t* box = boxes_c + (warp - 2) * S::kBox;
-        constexpr int esz = OUT == OUT_F32 ? 4 : 2;
-        constexpr bool kMx4Out = OUT == OUT_MX4 || OUT == OUT_MX4_GELU;
-        const bool vec_ok = (p.ldc * esz) % 32 == 0 && (uintptr_t)p.C % 32 == 0;
+        Mx4Epilogue<OUT, S::kCols> epi(p, &map_c, boxes_c + (warp - 2) * S::kBox, lane);
         const uint32_t t_addr = tmem + acc * BN + ((uint32_t)(quad * 32) << 16) + half * S::kCols;
         uint32_t use = 0;
         Mx4Walk walk;
         walk.init(blockIdx.x + acc * gridDim.x, 2 * gridDim.x, tiles_n);
         for (int t = blockIdx.x + acc * gridDim.x; t < total; t += 2 * gridDim.x, walk.next(), ++use) {
             const Mx4Rows q = mx4_rows(p, tb, walk);
-            const int first_col = walk.nt * BN + half * S::kCols, row = quad * 32 + lane;
-            const bool row_ok = row < q.rows;
-            // whole boxes by TMA (a dense C is cut off by the tensor map); the last rows of a segment row by row
-            const bool by_tma = p.tma_store && (!p.offsets || quad * 32 + 32 <= q.rows);
             mbar_wait_lean(&tmem_full_bar[acc], use & 1, dead, p.status);
             tc_fence_after();
-            if (by_tma) {
-                if (elect_one()) tma_store_wait_read();                  // the box before has left shared memory
-                __syncwarp();
-            }
+            epi.begin(walk.nt * BN + half * S::kCols, q.c_row + quad * 32, q.rows - quad * 32, walk.mt * kMx4Tile + quad * 32);
 #pragma unroll
-            for (int c = 0; c < kChunks; ++c) {
+            for (int c = 0; c < S::kCols / 32; ++c) {
                 float v[32];
                 tmem_load_32_nowait(t_addr + c * 32, (uint32_t*)v);
                 tmem_load_wait();
-                if (c == kChunks - 1) {
+                if (c == S::kCols / 32 - 1) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&tmem_empty_bar[acc]);
                 }
-                const int col0 = first_col + c * 32;
-                if (col0 >= p.N) continue;
-                if (OUT == OUT_BF16_GELU || OUT == OUT_MX4_GELU) {
-                    gelu_chunk(v);
-                } else if (OUT == OUT_BF16_ACT || ((OUT == OUT_F32 || OUT == OUT_MX4) && p.act != BIGMAC_ACT_IDENTITY)) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = act_apply(p.act, v[i]);
-                }
-                if constexpr (kMx4Out) {
-                    if (row_ok) store_block(p, v, walk.mt * kMx4Tile + row, col0 / 32);
-                    continue;
-                }
-                const int64_t off = (int64_t)(q.c_row + row) * p.ldc + col0;
-                if constexpr (OUT == OUT_F32) {
-                    if (!row_ok) continue;
-                    if (vec_ok && col0 + 32 <= p.N) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) st_global_32B((float*)p.C + off + 8 * i, (const uint32_t*)v + 8 * i);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (col0 + i < p.N) ((float*)p.C)[off + i] = v[i];
-                    }
-                } else {
-                uint32_t w[16];
-#pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-                if (by_tma) {
-                    stage_row<S::kCols>(box, lane, c, w);
-                } else if (row_ok) {
-                    if (vec_ok && col0 + 32 <= p.N) {
-                        st_global_32B((__nv_bfloat16*)p.C + off, w);
-                        st_global_32B((__nv_bfloat16*)p.C + off + 16, w + 8);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i)
-                            if (col0 + i < p.N) ((uint16_t*)p.C)[off + i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
-                    }
-                }
-                }
+                epi.chunk(c, v);
             }
-            if (by_tma && first_col < p.N) {
-                fence_async_smem();
-                __syncwarp();
-                if (elect_one()) {
-                    tma_store_2d(&map_c, box, first_col, q.c_row + quad * 32);
-                    tma_store_commit();
-                }
-            }
+            epi.end();
         }
-        if (elect_one()) tma_store_wait_read();                          // the boxes have left shared memory; the writes land before the grid ends
+        epi.finish();
     }
     tc_fence_before();
     __syncthreads();
@@ -434,6 +232,10 @@ cudaError_t launch_out(const Mx4View& a, const Mx4View& w, const Mx4Params& p, i
     return launch<BN, STAGES, OUT_BF16_ACT>(a, w, p, max_tiles_m, stream);
 }
 
+bool mx4_pair_pays(const Mx4View& a, const Mx4View& w, int sms) {
+    return !a.offsets && (int64_t)((a.rows + 255) / 256) * ((w.rows + 255) / 256) >= sms / 2 && a.K >= 512;
+}
+
 }  // namespace
 
 cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int dtype, void* c, int64_t ldc, const Mx4View* out, int* status,
@@ -446,6 +248,7 @@ cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int d
     p.act = act; p.status = status;
     const int64_t tiles_m = a.offsets ? a.capacity / kMx4Tile : (a.rows + kMx4Tile - 1) / kMx4Tile;
     const int sms = gemm_tc_sm_count();
+    if (mx4_pair_pays(a, w, sms)) return launch_mx4_matmul_pair(a, w, p, dtype, stream);
     if (tiles_m * ((p.N + 127) / 128) <= sms) return launch_out<64, 6>(a, w, p, dtype, tiles_m, stream);
     return launch_out<128, 4>(a, w, p, dtype, tiles_m, stream);
 }

@@ -1,0 +1,265 @@
+// Pieces that the products of microscaled 4-bit matrices share: instructions, the activation, what leaves a tile and how.
+#pragma once
+#include "tc_pair.cuh"
+#include "mx4.h"
+
+namespace bigmac {
+namespace mx4 {
+
+using namespace tc;
+
+constexpr int kSliceK = 256;                               // columns of a stage: one 128-byte row of codes
+constexpr uint32_t kABytes = 128 * 128;
+constexpr uint32_t kSfTile = 512;
+constexpr int kEpi = 16;                                   // epilogue warps, two sets with two to a lane quadrant
+constexpr int kThreadsMx4 = (2 + kEpi) * 32;
+
+struct Mx4Params {
+    void* C;
+    int64_t ldc;
+    const uint8_t *sa, *sw;                                // scale bytes
+    uint8_t *out_codes, *out_scales;                       // OUT_MX4: the result's
+    const int32_t* offsets;                                // grouped: the caller's table
+    int M, N, K, E;
+    int64_t capacity;                                      // rows that A has room for (grouped)
+    int act, tma_store;
+    int box_rows;                                          // of A's codes: a tile with few rows loads few
+    int* status;
+};
+
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");
+}
+// 512 bytes of scales, 32 rows of 16 bytes, to four columns of tensor memory in all four lane quadrants.
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+// Without swizzle: groups of 8 rows of 16 bytes, 128 bytes apart.
+__device__ __forceinline__ uint64_t scale_desc(uint32_t addr) {
+    return (uint64_t)((addr & 0x3ffff) >> 4) | ((uint64_t)(128 >> 4) << 32) | ((uint64_t)1 << 46);
+}
+__device__ __forceinline__ void umma_mx4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+        : "memory");
+}
+// Instruction descriptor: e2m1 x e2m1, scales ue8m0, M 128, N bn; `half`: which two of a column's four scale bytes.
+__host__ __device__ constexpr uint32_t instr_desc_mx4(int bn, int half) {
+    return ((uint32_t)(2 * half) << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(bn >> 3) << 17) | (1u << 23) | ((uint32_t)(128 >> 4) << 24) |
+           ((uint32_t)(2 * half) << 29);
+}
+
+// GELU of 32 accumulators for an output in bf16: z Phi(z), Phi(z) = sat(1/2 + z P(z^2)).  P is the minimax fit in the error of z Phi(z) on
+// |z| <= 4.5 (reweighted least squares on Chebyshev nodes), of even degree with a positive leading coefficient, so that behind 4.5 the
+// saturating multiply-add holds Phi at 0 or 1 without a look at the argument.  z Phi(z) is off by less than 3e-6 up to 4.5 and by less
+// than 3.3e-5 everywhere (at -4.5, where it is -1.5e-5 itself): a bf16 step of 1/2 is 4e-3.  Seven instructions an element; a form that
+// keeps the relative precision of the negative tail (a polynomial times an exponential) took twelve and, at 131072 rows of r 256, h 1024,
+// 96 us, erff 142.
+__device__ __forceinline__ void gelu_chunk(float* v) {
+    constexpr float kC[11] = {0.3989286422729492f, -0.06644835323095322f, 0.009928264655172825f, -0.0011627154890447855f, 0.00010752371599664912f, -7.800386811140925e-06f,
+                              4.3196823185098765e-07f, -1.7442022937075308e-08f, 4.790651764174925e-10f, -7.938010491981284e-12f, 5.954283154854453e-14f};
+    constexpr int kG = 8;                                  // pairs side by side, so that no multiply-add waits for the one before
+#pragma unroll
+    for (int g = 0; g < 16; g += kG) {
+        f32x2_t w[kG], P[kG];
+#pragma unroll
+        for (int i = 0; i < kG; ++i) {
+            const f32x2_t z = pk2(v[2 * (g + i)], v[2 * (g + i) + 1]);
+            w[i] = mul2(z, z);
+            P[i] = fma2(pk2(kC[10], kC[10]), w[i], pk2(kC[9], kC[9]));
+        }
+#pragma unroll
+        for (int k = 8; k >= 0; --k)
+#pragma unroll
+            for (int i = 0; i < kG; ++i) P[i] = fma2(P[i], w[i], pk2(kC[k], kC[k]));
+#pragma unroll
+        for (int i = 0; i < kG; ++i) {
+            float &z0 = v[2 * (g + i)], &z1 = v[2 * (g + i) + 1], p0, p1;
+            upk2(P[i], p0, p1);
+            upk2(mul2(pk2(z0, z1), pk2(fma_sat(z0, p0, 0.5f), fma_sat(z1, p1, 0.5f))), z0, z1);
+        }
+    }
+}
+
+// The tiles of a walker: t, t + step, ...  All columns of a row tile follow each other (its codes stay in L2).
+struct Mx4Tables {                                         // grouped: shared memory
+    const int32_t *prefix, *first, *end;                   // row tiles before expert e [E + 1]; its rows in the caller's order
+};
+struct Mx4Walk {
+    int mt, nt, e, step_m, step_n, tiles_n;
+    __device__ __forceinline__ void init(int t, int step, int n) {
+        tiles_n = n;
+        mt = t / n; nt = t - mt * n;
+        step_m = step / n; step_n = step - step_m * n;
+        e = 0;
+    }
+    __device__ __forceinline__ void next() {
+        mt += step_m; nt += step_n;
+        if (nt >= tiles_n) { nt -= tiles_n; ++mt; }
+    }
+    // The expert of row tile mt, which never falls from tile to tile.
+    __device__ __forceinline__ int expert(const Mx4Tables& tb, int E) {
+        while (e + 1 < E && tb.prefix[e + 1] <= mt) ++e;
+        return e;
+    }
+};
+struct Mx4Rows {
+    int expert, c_row, rows;                               // first row in C, rows of this tile that exist
+};
+__device__ __forceinline__ Mx4Rows mx4_rows(const Mx4Params& p, const Mx4Tables& tb, Mx4Walk& w) {
+    if (!p.offsets) return {0, w.mt * kMx4Tile, min(kMx4Tile, p.M - w.mt * kMx4Tile)};
+    const int e = w.expert(tb, p.E), c = tb.first[e] + (w.mt - tb.prefix[e]) * kMx4Tile;
+    return {e, c, min(kMx4Tile, tb.end[e] - c)};
+}
+
+// 32 columns of a row, packed, to the warp's box of 32 rows by COLS columns, laid out for a TMA store with the swizzle of its row's width.
+template <int COLS>
+__device__ __forceinline__ void stage_row(uint8_t* box, int lane, int chunk, const uint32_t* w) {
+    if (COLS == 64) {
+        uint8_t* row = box + lane * 128;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) st_shared_16B(row + (((chunk * 4 + j) ^ (lane & 7)) << 4), w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    } else {
+        stage_row_bf16(box, lane, w);
+    }
+}
+
+// 32 columns of a row are a block of the result in 4 bits: its scale and codes from the fp32 numbers, without a rounding between.
+__device__ __forceinline__ void store_block(const Mx4Params& p, float* v, int row, int block) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) top = max_nan(top, fabsf(v[i]));
+    const uint32_t s = mx4_scale_byte(top);
+    uint32_t c[4] = {0u, 0u, 0u, 0u};
+    if (s != 255u) {
+        const f32x2_t factor = mx4_factor2(s);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) upk2(mul2(pk2(v[2 * i], v[2 * i + 1]), factor), v[2 * i], v[2 * i + 1]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c[i] = mx4_e2m1x8(v + 8 * i);
+    }
+    *(uint4*)(p.out_codes + (int64_t)row * (p.N / 2) + block * 16) = make_uint4(c[0], c[1], c[2], c[3]);
+    uint8_t* at = p.out_scales + mx4_scale_at(row, block, mx4_ktiles(p.N));
+    *at = (uint8_t)s;
+    if (block + 1 == p.N / 32)
+        for (int b = block + 1; b & 3; ++b) *++at = 0;                   // behind the last block of the row
+}
+
+// What the epilogue does is fixed at compile time: with every way in one kernel its warps waited for instructions.
+enum { OUT_BF16 = 0, OUT_BF16_GELU, OUT_BF16_ACT, OUT_F32, OUT_MX4_GELU, OUT_MX4 };
+__host__ __device__ constexpr bool is_mx4_out(int out) { return out == OUT_MX4 || out == OUT_MX4_GELU; }
+
+// What an epilogue warp does with its 32 rows and COLS columns of a finished tile: 32 columns (a chunk) after each other.
+template <int OUT, int COLS>
+struct Mx4Epilogue {
+    static constexpr int kChunks = COLS / 32;
+    static constexpr uint32_t kBox = 32 * COLS * 2;
+    const Mx4Params& p;
+    const CUtensorMap* map_c;
+    uint8_t* box;
+    int lane;
+    bool vec_ok;
+    // the tile's
+    int first_col, row0, rows, a_row0;                     // column, first of the warp's rows in C, how many exist, their place in A
+    bool by_tma, by_rows;
+
+    __device__ __forceinline__ Mx4Epilogue(const Mx4Params& p_, const CUtensorMap* map, uint8_t* box_, int lane_) : p(p_), map_c(map), box(box_), lane(lane_) {
+        constexpr int esz = OUT == OUT_F32 ? 4 : 2;
+        vec_ok = (p.ldc * esz) % 32 == 0 && (uintptr_t)p.C % 32 == 0;
+    }
+    // Whole boxes leave by TMA (a dense C is cut off by the tensor map), the last rows of a segment row by row, rows that are not on 16-byte boundaries
+    // through the box, too, a row after the other (lanes that each wrote their own row element by element took 20 times as long).
+    __device__ __forceinline__ void begin(int first_col_, int row0_, int rows_, int a_row0_) {
+        first_col = first_col_; row0 = row0_; rows = rows_; a_row0 = a_row0_;
+        by_tma = OUT <= OUT_BF16_ACT && p.tma_store && (!p.offsets || rows >= 32);
+        by_rows = OUT <= OUT_BF16_ACT && !by_tma && !vec_ok;
+        if (OUT <= OUT_BF16_ACT) {
+            if (elect_one()) tma_store_wait_read();        // the box before has left shared memory
+            __syncwarp();
+        }
+    }
+    __device__ __forceinline__ void chunk(int c, float* v) {
+        const int col0 = first_col + c * 32;
+        if (col0 >= p.N) return;
+        if (OUT == OUT_BF16_GELU || OUT == OUT_MX4_GELU) {
+            gelu_chunk(v);
+        } else if (OUT == OUT_BF16_ACT || ((OUT == OUT_F32 || OUT == OUT_MX4) && p.act != BIGMAC_ACT_IDENTITY)) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = act_apply(p.act, v[i]);
+        }
+        if constexpr (is_mx4_out(OUT)) {
+            if (lane < rows) store_block(p, v, a_row0 + lane, col0 / 32);
+        } else if constexpr (OUT == OUT_F32) {
+            if (lane >= rows) return;
+            float* to = (float*)p.C + (int64_t)(row0 + lane) * p.ldc + col0;
+            if (vec_ok && col0 + 32 <= p.N) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) st_global_32B(to + 8 * i, (const uint32_t*)v + 8 * i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (col0 + i < p.N) to[i] = v[i];
+            }
+        } else {
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+            if (by_tma || by_rows) {
+                stage_row<COLS>(box, lane, c, w);
+            } else if (lane < rows) {
+                __nv_bfloat16* to = (__nv_bfloat16*)p.C + (int64_t)(row0 + lane) * p.ldc + col0;
+                if (col0 + 32 <= p.N) {
+                    st_global_32B(to, w);
+                    st_global_32B(to + 16, w + 8);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (col0 + i < p.N) ((uint16_t*)to)[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void end() {
+        if (OUT > OUT_BF16_ACT || first_col >= p.N) return;
+        if (by_tma) {
+            fence_async_smem();
+            __syncwarp();
+            if (elect_one()) {
+                tma_store_2d(map_c, box, first_col, row0);
+                tma_store_commit();
+            }
+        } else if (by_rows) {
+            __syncwarp();
+            constexpr int kAtOnce = 64 / COLS;             // rows that 32 lanes with two columns each cover
+            const int sub = kAtOnce == 2 ? lane >> 4 : 0, pair = kAtOnce == 2 ? lane & 15 : lane;
+            const bool words = p.ldc % 2 == 0 && (uintptr_t)p.C % 4 == 0;
+            const int n = min(rows, 32), col = first_col + 2 * pair;
+            for (int r = sub; r < n; r += kAtOnce) {
+                const int piece = COLS == 64 ? (pair >> 2) ^ (r & 7) : (pair >> 2) ^ ((r >> 1) & 3);
+                const uint32_t w = *(const uint32_t*)(box + r * COLS * 2 + piece * 16 + (pair & 3) * 4);
+                uint16_t* to = (uint16_t*)p.C + (int64_t)(row0 + r) * p.ldc + col;
+                if (words && col + 2 <= p.N) {
+                    *(uint32_t*)to = w;
+                } else {
+                    if (col < p.N) to[0] = (uint16_t)w;
+                    if (col + 1 < p.N) to[1] = (uint16_t)(w >> 16);
+                }
+            }
+            __syncwarp();                                  // the box is read: the next tile's rows may go in
+        }
+    }
+    __device__ __forceinline__ void finish() {
+        if (OUT <= OUT_BF16_ACT && elect_one()) tma_store_wait_read();   // the boxes have left shared memory; the writes land before the grid ends
+    }
+};
+
+}  // namespace mx4
+
+// Dense products of many 256 x 256 tiles (gemm_mx4_pair.cu).
+cudaError_t launch_mx4_matmul_pair(const Mx4View& a, const Mx4View& w, const mx4::Mx4Params& p, int dtype, cudaStream_t stream);
+
+}  // namespace bigmac

@@ -136,6 +136,23 @@ def test_product(binding, M, N, K, dtype):
     assert binding.operator_status() == 0
 
 
+# enough 256 x 256 tiles for CTA pairs: an odd number of row tiles, ragged columns and K tiles, rows that are no multiple of 16 bytes
+@pytest.mark.parametrize("M,N,K", [(2400, 2000, 544), (4700, 1111, 1056), (2304, 2304, 512), (19000, 200, 640)])
+def test_product_on_cta_pairs(binding, M, N, K):
+    rng = _gen(M + N + K)
+    x64 = np.round(rng.standard_normal((M, K)) * 16) / 16
+    wc, wb, codes, scales = _weights(rng, (), N, K)
+    q, W = binding.mx4_quantize(torch.from_numpy(x64).to(torch.bfloat16).cuda()), binding.Mx4(codes, scales)
+    a, w = ref.values(*ref.quantise(x64)), ref.values(wc, wb)
+    for act, dtype in ((3, torch.float32), (3, torch.bfloat16), (1, torch.bfloat16), (0, torch.bfloat16)):
+        out = torch.full((M + 1, N), 5.0, dtype=dtype, device="cuda")
+        binding.mx4_matmul(q, W, act=act, out=out[:M])
+        _check_product(out[:M], a, w, act, dtype)
+        assert bool((out[M] == 5.0).all())
+    assert torch.equal(out[:M], binding.mx4_matmul(q, W, act=0))
+    assert binding.operator_status() == 0
+
+
 @pytest.mark.parametrize("act", [0, 1, 2])
 def test_product_with_activation(binding, act):
     rng = _gen(act)
@@ -231,7 +248,7 @@ def test_grouped_rows_in_no_segment_are_left(binding):
 
 
 @pytest.mark.parametrize("act", [0, 1, 2, 3])
-@pytest.mark.parametrize("E,rows,N,K", [(0, 1, 32, 64), (0, 300, 160, 256), (0, 1000, 1024, 128), (0, 2600, 4096, 64), (8, 700, 96, 96), (64, 512, 1024, 256)])
+@pytest.mark.parametrize("E,rows,N,K", [(0, 1, 32, 64), (0, 300, 160, 256), (0, 1000, 1024, 128), (0, 2600, 4096, 64), (0, 2400, 2048, 512), (8, 700, 96, 96), (64, 512, 1024, 256)])
 def test_product_in_4_bits(binding, E, rows, N, K, act):
     """The result's values are roundings of act(a w^T): a block's scale is that of its largest magnitude, a code off by half a step of its
     place (or more where the fp32 value lies next to a border: then the neighbour's half step), magnitudes above 6 scales at 6."""
