@@ -78,6 +78,8 @@ const char *bigmac_profile_slot_name(int slot);
  *   "overlap" 0/1        backward pass on one stream / independent launches on the handle's second stream (default 1)
  *   "tc_pair" 0/1        never / where faster: the CTA-pair tcgen05 kernel (default 1)
  *   "groupk" 0/1         never / where it pays: the dynamically scheduled per-expert weight-gradient kernel (default 1)
+ *   "mx4_tile" 0/64/128/256  columns of a tile of the 4-bit products, 256 on CTA pairs and for dense ones only (default 0: by
+ *                        the sizes)
  *   "ffn" 0/1/2          both contractions of an expert in one kernel never / where it pays / wherever it can (default 1); read when a
  *                        handle is created
  *   "fused_mlp" 0/1/2    inference expert GEMM1 + sigma + GEMM2 in one kernel never / on short tile lists / always (default 1)

@@ -232,8 +232,15 @@ cudaError_t launch_out(const Mx4View& a, const Mx4View& w, const Mx4Params& p, i
     return launch<BN, STAGES, OUT_BF16_ACT>(a, w, p, max_tiles_m, stream);
 }
 
-bool mx4_pair_pays(const Mx4View& a, const Mx4View& w, int sms) {
-    return !a.offsets && (int64_t)((a.rows + 255) / 256) * ((w.rows + 255) / 256) >= sms / 2 && a.K >= 512;
+// Which tiles.  64 columns as long as every SM gets one tile at most: a CTA's loads are what few tiles wait for (one row, N 4096, K 4096 6.7 us
+// against 7.0 with 128; 300 rows of N 4096, two rounds, 11.4 against 7.8).  CTA pairs for dense products of more than a round of 128 x 128
+// tiles that are long enough for the pair's longer start and its single accumulator: us with 128 columns / pairs, t tiles of 128 x 128:
+// t 256: K 512 4.9 / 5.8, K 1024 6.4 / 6.4, K 4096 12.8 / 10.1; t 512: K 256 6.5 / 6.6, K 512 7.2 / 7.0; t 1024: K 256 9.1 / 8.7; t 4096, K 4096
+// 74 / 54.
+int mx4_tile_of(const Mx4View& a, const Mx4View& w, int64_t tiles_m, int sms) {
+    const int64_t tiles = tiles_m * ((w.rows + 127) / 128);
+    if (tiles_m * ((w.rows + 63) / 64) <= sms) return 64;
+    return !a.offsets && tiles > sms && tiles * a.K >= 1 << 18 ? 256 : 128;
 }
 
 }  // namespace
@@ -248,9 +255,10 @@ cudaError_t launch_mx4_matmul(const Mx4View& a, const Mx4View& w, int act, int d
     p.act = act; p.status = status;
     const int64_t tiles_m = a.offsets ? a.capacity / kMx4Tile : (a.rows + kMx4Tile - 1) / kMx4Tile;
     const int sms = gemm_tc_sm_count();
-    if (mx4_pair_pays(a, w, sms)) return launch_mx4_matmul_pair(a, w, p, dtype, stream);
-    if (tiles_m * ((p.N + 127) / 128) <= sms) return launch_out<64, 6>(a, w, p, dtype, tiles_m, stream);
-    return launch_out<128, 4>(a, w, p, dtype, tiles_m, stream);
+    int tile = switches().mx4_tile;
+    if (tile != 64 && tile != 128 && (tile != 256 || a.offsets)) tile = mx4_tile_of(a, w, tiles_m, sms);
+    if (tile == 256) return launch_mx4_matmul_pair(a, w, p, dtype, stream);
+    return tile == 64 ? launch_out<64, 6>(a, w, p, dtype, tiles_m, stream) : launch_out<128, 4>(a, w, p, dtype, tiles_m, stream);
 }
 
 }  // namespace bigmac

@@ -175,7 +175,7 @@ struct Mx4Epilogue {
     // through the box, too, a row after the other (lanes that each wrote their own row element by element took 20 times as long).
     __device__ __forceinline__ void begin(int first_col_, int row0_, int rows_, int a_row0_) {
         first_col = first_col_; row0 = row0_; rows = rows_; a_row0 = a_row0_;
-        by_tma = OUT <= OUT_BF16_ACT && p.tma_store && (!p.offsets || rows >= 32);
+        by_tma = OUT <= OUT_BF16_ACT && p.tma_store && (rows >= 32 || !p.offsets);
         by_rows = OUT <= OUT_BF16_ACT && !by_tma && !vec_ok;
         if (OUT <= OUT_BF16_ACT) {
             if (elect_one()) tma_store_wait_read();        // the box before has left shared memory
@@ -184,7 +184,7 @@ struct Mx4Epilogue {
     }
     __device__ __forceinline__ void chunk(int c, float* v) {
         const int col0 = first_col + c * 32;
-        if (col0 >= p.N) return;
+        if (col0 >= p.N || rows <= 0) return;              // nothing of the tile is here: a warp's 32 rows may lie behind a segment's last
         if (OUT == OUT_BF16_GELU || OUT == OUT_MX4_GELU) {
             gelu_chunk(v);
         } else if (OUT == OUT_BF16_ACT || ((OUT == OUT_F32 || OUT == OUT_MX4) && p.act != BIGMAC_ACT_IDENTITY)) {
@@ -224,7 +224,7 @@ struct Mx4Epilogue {
         }
     }
     __device__ __forceinline__ void end() {
-        if (OUT > OUT_BF16_ACT || first_col >= p.N) return;
+        if (OUT > OUT_BF16_ACT || first_col >= p.N || rows <= 0) return;
         if (by_tma) {
             fence_async_smem();
             __syncwarp();

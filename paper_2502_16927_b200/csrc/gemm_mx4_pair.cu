@@ -159,7 +159,6 @@ gemm_mx4_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive_cluster(leader_empty);
-            if (row0 >= p.M) continue;                                   // the second CTA's rows of a last odd row tile
             epi.begin(col0, row0, p.M - row0, row0);
             epi.chunk(0, v[0]);
             epi.chunk(1, v[1]);
