@@ -372,7 +372,7 @@ def _here() -> int:
 
 
 def _dense(t: torch.Tensor, name: str, here: int) -> int:
-    if t.get_device() != here or not t.is_contiguous():
+    if t.get_device() != here or here < 0 or not t.is_contiguous():
         raise ValueError(f"{name}: a dense tensor on the current device, cuda:{here}, is needed")
     return t.data_ptr()
 
@@ -531,34 +531,41 @@ def residual_norm_backward(x, y, gate, post, pre, dr, dn, stats, G: Optional[Dic
     return dx, dy, dgate
 
 
-class Mx4(NamedTuple):
+class Mx4:
     """A matrix in microscaled 4-bit floating point (bigmac_mx4_t): codes [rows, K / 2] and scales [row tiles, K tiles, 512] of one
-    matrix, both with a leading E for the stacked weights of E experts; with `offsets` the segments of a routing's experts, `rows`
-    rows in the caller's order."""
-    codes: torch.Tensor
-    scales: torch.Tensor
-    offsets: Optional[torch.Tensor] = None
-    rows: Optional[int] = None
+    matrix, both with a leading E for the stacked weights of E experts; with `offsets` (int32 [E + 1]) the segments of a routing's
+    experts, `rows` rows in the caller's order."""
+    __slots__ = ("codes", "scales", "offsets", "rows", "_c", "_device")
+
+    def __init__(self, codes: torch.Tensor, scales: torch.Tensor, offsets: Optional[torch.Tensor] = None, rows: Optional[int] = None):
+        shape = codes.shape
+        stored, half, E = shape[-2] if len(shape) > 1 else 0, shape[-1], shape[0] if len(shape) == 3 else 0
+        tiles = (-(-stored // 128), -(-half // 64), 512)
+        if (codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or not 1 < len(shape) < 4 or
+                scales.shape != (tiles if len(shape) == 2 else (E, *tiles))):
+            raise ValueError(f"Mx4: codes [rows, K / 2] and scales [row tiles, K tiles, 512] of torch.uint8, or both with a leading E; not "
+                             f"{tuple(shape)} and {tuple(scales.shape)}")
+        device, table = codes.get_device(), None
+        if offsets is None:
+            rows = stored
+        else:
+            if E or rows is None:
+                raise ValueError("a grouped Mx4 has codes of two dimensions and rows")
+            E, table = _offsets(offsets, device), offsets.data_ptr()
+            if stored < _mx4_stored(rows, E):
+                raise ValueError(f"Mx4: {rows} rows of {E} experts need {_mx4_stored(rows, E)} rows of codes")
+        self._keep(codes, scales, offsets, rows, device,
+                   bigmac_mx4_t(_dense(codes, "codes", device), _dense(scales, "scales", device), rows, 2 * half, E, table))
+
+    def _keep(self, codes, scales, offsets, rows, device, c):
+        self.codes, self.scales, self.offsets, self.rows, self._device, self._c = codes, scales, offsets, rows, device, c
+        return self
 
 
 def _mx4(q: Mx4, here: int) -> bigmac_mx4_t:
-    codes, scales, offsets, rows = q
-    shape = codes.shape
-    stored, half, E = shape[-2] if len(shape) > 1 else 0, shape[-1], shape[0] if len(shape) == 3 else 0
-    tiles = (-(-stored // 128), -(-half // 64), 512)
-    if (codes.dtype is not torch.uint8 or scales.dtype is not torch.uint8 or not 1 < len(shape) < 4 or
-            scales.shape != (tiles if len(shape) == 2 else (E, *tiles))):
-        raise ValueError(f"Mx4: codes [rows, K / 2] and scales [row tiles, K tiles, 512] of torch.uint8, or both with a leading E; not "
-                         f"{tuple(shape)} and {tuple(scales.shape)}")
-    if offsets is None:
-        rows = stored
-    else:
-        if E or rows is None:
-            raise ValueError("a grouped Mx4 has codes of two dimensions and rows")
-        E = _offsets(offsets, here)
-        if stored < _mx4_stored(rows, E):
-            raise ValueError(f"Mx4: {rows} rows of {E} experts need {_mx4_stored(rows, E)} rows of codes")
-    return bigmac_mx4_t(_dense(codes, "codes", here), _dense(scales, "scales", here), rows, 2 * half, E, None if offsets is None else offsets.data_ptr())
+    if q._device != here:
+        raise ValueError(f"Mx4 on cuda:{q._device}, the current device is cuda:{here}")
+    return q._c
 
 
 def _mx4_stored(rows: int, E: int) -> int:
@@ -594,7 +601,7 @@ def mx4_quantize(x: torch.Tensor, offsets: Optional[torch.Tensor] = None, slot_o
     codes, scales = _empty_mx4(stored, K, x.device)
     q = bigmac_mx4_t(codes.data_ptr(), scales.data_ptr(), rows, K, E, table)
     _check(lib().bigmac_mx4_quantize(ptr, _dtype(x.dtype), x_rows, ld, slots, k, C.byref(q), _stream()), "bigmac_mx4_quantize")
-    return Mx4(codes, scales, offsets, rows)
+    return Mx4.__new__(Mx4)._keep(codes, scales, offsets, rows, here, q)
 
 
 def _output(out, rows: int, columns: int, dtype, device, here: int):
@@ -640,7 +647,7 @@ def mx4_matmul_mx4(a: Mx4, w: Mx4, act: int = 3) -> Mx4:
     codes, scales = _empty_mx4(a.codes.shape[0], cw.rows, a.codes.device)
     out = bigmac_mx4_t(codes.data_ptr(), scales.data_ptr(), ca.rows, cw.rows, ca.E, ca.offsets)
     _check(lib().bigmac_mx4_matmul_mx4(C.byref(ca), C.byref(cw), act, C.byref(out), _stream()), "bigmac_mx4_matmul_mx4")
-    return Mx4(codes, scales, a.offsets, a.rows)
+    return Mx4.__new__(Mx4)._keep(codes, scales, a.offsets, a.rows, here, out)
 
 
 def mx4_quantize_weights(w: torch.Tensor) -> Mx4:

@@ -30,7 +30,7 @@ struct Mx4Smem {
     static constexpr int kCols = BN / 2;                                 // columns of an epilogue warp
     static constexpr uint32_t kBox = 32 * kCols * 2;
     static constexpr uint32_t kBars = (2 * STAGES + 4) * 8 + 16;
-    static constexpr size_t bytes(int E) { return 1024 + STAGES * kStage + kEpi * kBox + kBars + (size_t)(3 * E + 1) * 4; }
+    static constexpr size_t bytes(int E) { return 1024 + STAGES * kStage + kEpi * kBox + kBars + (size_t)(2 * E + 2) * 4; }
 };
 
 template <int BN, int STAGES, int OUT>
@@ -50,7 +50,6 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     uint32_t* tmem_slot = (uint32_t*)(tmem_empty_bar + 2);
     volatile int* dead = (volatile int*)(tmem_slot + 1);
     int32_t* tables = (int32_t*)(tmem_slot + 4);
-    const Mx4Tables tb{tables, tables + p.E + 1, tables + 2 * p.E + 1};
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (threadIdx.x == 32) {
@@ -70,21 +69,20 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     __syncthreads();
     grid_dependency_launch();
     grid_dependency_wait();
-    if (p.offsets) {
-        if (warp == 2) mx4_tile_prefix(p.offsets, p.E, p.M, tables);
-        for (int e = (int)threadIdx.x - 96; e >= 0 && e < p.E; e += kThreadsMx4 - 96) {
-            const Mx4Segment seg = mx4_segment(p.offsets, e, p.M);
-            tables[p.E + 1 + e] = seg.first;
-            tables[2 * p.E + 1 + e] = seg.first + seg.count;
-        }
-        __syncthreads();
-    }
+    Mx4Segments seg{};
+    if (p.offsets) seg.load(tables, p.offsets, p.E, p.M);
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     const int ktiles = mx4_ktiles(p.K), num_kb = (p.K + kSliceK - 1) / kSliceK;
     const int tiles_n = (p.N + BN - 1) / BN;
-    const int tiles_m = p.offsets ? (int)min((int64_t)tb.prefix[p.E], p.capacity / kMx4Tile) : (p.M + kMx4Tile - 1) / kMx4Tile;
+    const int tiles_m = p.offsets ? (int)min((int64_t)seg.tiles[p.E], p.capacity / kMx4Tile) : (p.M + kMx4Tile - 1) / kMx4Tile;
     const int total = tiles_m * tiles_n;
+    // The CTAs side by side along rows of tiles, which share their codes in L2; grouped with few tiles a CTA: a run of tiles each, so that an expert is
+    // looked up once (a step of the grid crosses 18 of 64 experts at 1024 columns: 512 rows 10.8 us, in runs 9.5).  With more, runs spread the CTAs
+    // over more weights than L2 holds (65536 rows of 128 experts, h 2048 -> r 512, 16 tiles a CTA: 57 us, in runs 69).
+    const bool runs = p.offsets && total <= 4 * (int)gridDim.x;
+    const int first = runs ? (int)((int64_t)total * blockIdx.x / gridDim.x) : (int)blockIdx.x, step = runs ? 1 : (int)gridDim.x;
+    const int last = runs ? (int)((int64_t)total * (blockIdx.x + 1) / gridDim.x) : total;
 
     if (warp == 0) {
         // ------------------------------------------------------------------ producer
@@ -92,9 +90,9 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             const int w_row_tiles = (p.N + 127) / 128;
             uint32_t s = 0, phase = 1;
             Mx4Walk walk;
-            walk.init(blockIdx.x, gridDim.x, tiles_n);
-            for (int t = blockIdx.x; t < total; t += gridDim.x, walk.next()) {
-                const Mx4Rows q = mx4_rows(p, tb, walk);
+            walk.init(first, step, tiles_n);
+            for (int t = first; t < last; t += step, walk.next()) {
+                const Mx4Rows q = mx4_rows(p, seg, walk);
                 const int a_row = walk.mt * kMx4Tile, n0 = walk.nt * BN, wt = n0 / 128;
                 const uint8_t* sa = p.sa + (int64_t)walk.mt * ktiles * kSfTile;
                 const uint8_t* sw = p.sw + ((int64_t)q.expert * w_row_tiles + wt) * ktiles * kSfTile;
@@ -122,7 +120,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             const uint64_t da0 = smem_desc(smem_u32(smem), 16, 1024), db0 = smem_desc(smem_u32(smem + kABytes), 16, 1024);
             const uint64_t df0 = scale_desc(smem_u32(smem + kABytes + S::kBBytes));
             uint32_t stage = 0, phase = 0, local = 0;
-            for (int t = blockIdx.x; t < total; t += gridDim.x, ++local) {
+            for (int t = first; t < last; t += step, ++local) {
                 const uint32_t acc = local & 1, use = local >> 1;
                 // a 64-column tile in the second half of W's row tile: its rows' bytes start two columns further
                 const uint32_t shift = BN == 64 ? (uint32_t)((t % tiles_n) & 1) * 2 : 0;
@@ -163,9 +161,9 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         const uint32_t t_addr = tmem + acc * BN + ((uint32_t)(quad * 32) << 16) + half * S::kCols;
         uint32_t use = 0;
         Mx4Walk walk;
-        walk.init(blockIdx.x + acc * gridDim.x, 2 * gridDim.x, tiles_n);
-        for (int t = blockIdx.x + acc * gridDim.x; t < total; t += 2 * gridDim.x, walk.next(), ++use) {
-            const Mx4Rows q = mx4_rows(p, tb, walk);
+        walk.init(first + (int)acc * step, 2 * step, tiles_n);
+        for (int t = first + (int)acc * step; t < last; t += 2 * step, walk.next(), ++use) {
+            const Mx4Rows q = mx4_rows(p, seg, walk);
             mbar_wait_lean(&tmem_full_bar[acc], use & 1, dead, p.status);
             tc_fence_after();
             epi.begin(walk.nt * BN + half * S::kCols, q.c_row + quad * 32, q.rows - quad * 32, walk.mt * kMx4Tile + quad * 32);

@@ -86,34 +86,32 @@ __device__ __forceinline__ void gelu_chunk(float* v) {
 }
 
 // The tiles of a walker: t, t + step, ...  All columns of a row tile follow each other (its codes stay in L2).
-struct Mx4Tables {                                         // grouped: shared memory
-    const int32_t *prefix, *first, *end;                   // row tiles before expert e [E + 1]; its rows in the caller's order
-};
 struct Mx4Walk {
     int mt, nt, e, step_m, step_n, tiles_n;
     __device__ __forceinline__ void init(int t, int step, int n) {
         tiles_n = n;
         mt = t / n; nt = t - mt * n;
         step_m = step / n; step_n = step - step_m * n;
-        e = 0;
+        e = -1;
     }
     __device__ __forceinline__ void next() {
         mt += step_m; nt += step_n;
         if (nt >= tiles_n) { nt -= tiles_n; ++mt; }
     }
     // The expert of row tile mt, which never falls from tile to tile.
-    __device__ __forceinline__ int expert(const Mx4Tables& tb, int E) {
-        while (e + 1 < E && tb.prefix[e + 1] <= mt) ++e;
+    __device__ __forceinline__ int expert(const Mx4Segments& seg) {
+        if (e < 0) e = mx4_find(seg.tiles, seg.E, mt);
+        while (e + 1 < seg.E && seg.tiles[e + 1] <= mt) ++e;
         return e;
     }
 };
 struct Mx4Rows {
     int expert, c_row, rows;                               // first row in C, rows of this tile that exist
 };
-__device__ __forceinline__ Mx4Rows mx4_rows(const Mx4Params& p, const Mx4Tables& tb, Mx4Walk& w) {
+__device__ __forceinline__ Mx4Rows mx4_rows(const Mx4Params& p, const Mx4Segments& seg, Mx4Walk& w) {
     if (!p.offsets) return {0, w.mt * kMx4Tile, min(kMx4Tile, p.M - w.mt * kMx4Tile)};
-    const int e = w.expert(tb, p.E), c = tb.first[e] + (w.mt - tb.prefix[e]) * kMx4Tile;
-    return {e, c, min(kMx4Tile, tb.end[e] - c)};
+    const int e = w.expert(seg), within = (w.mt - seg.tiles[e]) * kMx4Tile;
+    return {e, seg.offsets[e] + within, min(kMx4Tile, seg.count(e) - within)};
 }
 
 // 32 columns of a row, packed, to the warp's box of 32 rows by COLS columns, laid out for a TMA store with the swizzle of its row's width.

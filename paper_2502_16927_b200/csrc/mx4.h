@@ -23,27 +23,36 @@ inline int64_t mx4_padded_rows(int64_t rows, int E) {
 }
 
 #ifdef __CUDACC__
-// Rows of expert e by the caller's table, as far as they lie in [0, rows): a table that is none reads and writes nothing outside.
-struct Mx4Segment { int first, count; };
-__device__ __forceinline__ Mx4Segment mx4_segment(const int32_t* __restrict__ offsets, int e, int rows) {
-    const int a = min(max(offsets[e], 0), rows), b = min(max(offsets[e + 1], a), rows);
-    return {a, b - a};
-}
-// out[e] = tiles of the experts before e, e = 0 .. E; all threads of a warp.
-__device__ __forceinline__ void mx4_tile_prefix(const int32_t* __restrict__ offsets, int E, int rows, int32_t* out) {
-    const int lane = threadIdx.x & 31, per = (E + 31) / 32, e0 = min(E, lane * per), e1 = min(E, e0 + per);
-    int mine = 0;
-    for (int e = e0; e < e1; ++e) mine += (mx4_segment(offsets, e, rows).count + kMx4Tile - 1) / kMx4Tile;
-    int run = mine;
+// The segments of a grouped matrix in shared memory, 2 E + 2 words: the caller's table cut to [0, rows], so that a table that is none reads and
+// writes nothing outside, and the row tiles before every expert.  All threads of a block call it.
+struct Mx4Segments {
+    const int32_t *offsets, *tiles;    // [E + 1] each
+    int E;
+    __device__ __forceinline__ void load(int32_t* smem, const int32_t* __restrict__ table, int E_, int rows) {
+        int32_t* cut = smem;
+        int32_t* before = smem + E_ + 1;
+        offsets = cut; tiles = before; E = E_;
+        for (int e = threadIdx.x; e <= E; e += blockDim.x) cut[e] = min(max(table[e], 0), rows);
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            const int lane = threadIdx.x, per = (E + 31) / 32, e0 = min(E, lane * per), e1 = min(E, e0 + per);
+            int mine = 0;
+            for (int e = e0; e < e1; ++e) mine += tiles_of(e);
+            int run = mine;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int a = __shfl_up_sync(0xffffffffu, run, o);
-        if (lane >= o) run += a;
+            for (int o = 1; o < 32; o <<= 1) {
+                const int a = __shfl_up_sync(0xffffffffu, run, o);
+                if (lane >= o) run += a;
+            }
+            if (lane == 31) before[E] = run;
+            run -= mine;
+            for (int e = e0; e < e1; ++e) { before[e] = run; run += tiles_of(e); }
+        }
+        __syncthreads();
     }
-    if (lane == 31) out[E] = run;
-    run -= mine;
-    for (int e = e0; e < e1; ++e) { out[e] = run; run += (mx4_segment(offsets, e, rows).count + kMx4Tile - 1) / kMx4Tile; }
-}
+    __device__ __forceinline__ int count(int e) const { return max(offsets[e + 1] - offsets[e], 0); }
+    __device__ __forceinline__ int tiles_of(int e) const { return (count(e) + kMx4Tile - 1) / kMx4Tile; }
+};
 // The last e in [0, E) with table[e] <= v; table ascending, table[0] <= v.
 __device__ __forceinline__ int mx4_find(const int32_t* table, int E, int v) {
     int lo = 0, hi = E - 1;

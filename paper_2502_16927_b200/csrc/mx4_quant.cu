@@ -22,30 +22,19 @@ constexpr int kThreads = 256;
 
 // Where row i of the caller's order lies in the matrix; -1: in no segment.
 struct RowMap {
-    const int32_t *first, *tiles, *end;   // of the experts' segments, shared memory
-    int E;
+    Mx4Segments seg;
     int64_t capacity;
+    __device__ __forceinline__ RowMap(const Mx4View& q, int32_t* smem) : capacity(q.capacity) {
+        seg.E = 0;
+        if (q.offsets) seg.load(smem, q.offsets, q.E, q.rows);
+    }
     __device__ __forceinline__ int at(int i) const {
-        if (E == 0) return i;
-        const int e = mx4_find(first, E, i);
-        const int64_t row = (int64_t)tiles[e] * kMx4Tile + (i - first[e]);
-        return i >= first[e] && i < end[e] && row < capacity ? (int)row : -1;
+        if (seg.E == 0) return i;
+        const int e = mx4_find(seg.offsets, seg.E, i), within = i - seg.offsets[e];
+        const int64_t row = (int64_t)seg.tiles[e] * kMx4Tile + within;
+        return within >= 0 && within < seg.count(e) && row < capacity ? (int)row : -1;
     }
 };
-
-__device__ __forceinline__ RowMap load_map(const Mx4View& q, int32_t* smem) {
-    RowMap m{smem, smem + q.E, smem + 2 * q.E + 1, q.offsets ? q.E : 0, q.capacity};
-    if (m.E) {
-        for (int e = threadIdx.x; e < q.E; e += blockDim.x) {
-            const Mx4Segment s = mx4_segment(q.offsets, e, q.rows);
-            smem[e] = s.first;
-            smem[2 * q.E + 1 + e] = s.first + s.count;
-        }
-        if (threadIdx.x < 32) mx4_tile_prefix(q.offsets, q.E, q.rows, smem + q.E);
-        __syncthreads();
-    }
-    return m;
-}
 
 // The work is cut into units: up to 1024 columns (a warp's 32 a lane) of a row.  A warp takes chunks of 32 units at most, one after the other over the
 // grid, a pass of as many units as its lanes have room for at a time.
@@ -132,7 +121,7 @@ __global__ void __launch_bounds__(kThreads, 5) mx4_quantize_kernel(const T* __re
     extern __shared__ int32_t smem[];
     grid_dependency_launch();
     grid_dependency_wait();
-    const RowMap map = load_map(q, smem);
+    const RowMap map(q, smem);
     const int blocks = q.K / 32, ktiles = mx4_ktiles(q.K);
     const Chunks c(q.rows, q.K, lanes_log2, chunk);
     for (int64_t base = c.first; base < c.units; base += c.step) {
@@ -199,7 +188,7 @@ __global__ void __launch_bounds__(kThreads) mx4_dequantize_kernel(Mx4View q, T* 
     extern __shared__ int32_t smem[];
     grid_dependency_launch();
     grid_dependency_wait();
-    const RowMap map = load_map(q, smem);
+    const RowMap map(q, smem);
     const int blocks = q.K / 32, ktiles = mx4_ktiles(q.K);
     const Chunks c(q.rows, q.K, lanes_log2, chunk);
     for (int64_t base = c.first; base < c.units; base += c.step) {
@@ -268,7 +257,7 @@ struct Shape {
 };
 // Do rows allow 32-byte accesses?
 bool rows_by_32(const void* p, int dtype, int64_t ld) { return (uintptr_t)p % 32 == 0 && ld * (dtype == BIGMAC_BF16 ? 2 : 4) % 32 == 0; }
-size_t map_bytes(const Mx4View& q) { return q.offsets ? (size_t)(3 * q.E + 1) * 4 : 0; }
+size_t map_bytes(const Mx4View& q) { return q.offsets ? (size_t)(2 * q.E + 2) * 4 : 0; }
 
 }  // namespace
 

@@ -324,3 +324,29 @@ def test_captured_and_on_another_stream(binding):
         other = binding.mx4_matmul(binding.mx4_quantize(x), W, dtype=torch.float32)
         _check_product(y, ref.values(*ref.quantise(x64)), ref.values(wc, wb), 3, torch.float32)
         assert torch.equal(y, other)
+
+
+def test_binding_refuses_what_is_no_4_bit_matrix(binding):
+    u8 = dict(dtype=torch.uint8, device="cuda")
+    i32 = dict(dtype=torch.int32, device="cuda")
+    ok = torch.zeros(4, 32, **u8), torch.zeros(1, 1, 512, **u8)
+    binding.Mx4(*ok)
+    for codes, scales, kw in ((torch.zeros(4, 32, device="cuda"), ok[1], {}), (ok[0], torch.zeros(1, 2, 512, **u8), {}), (ok[0], ok[1].cpu(), {}),
+                              (torch.zeros(129, 32, **u8), ok[1], {}), (torch.zeros(2, 4, 32, **u8), ok[1], {}), (torch.zeros(4, 64, **u8)[:, :32], ok[1], {}),
+                              (*ok, dict(offsets=torch.zeros(3, **i32))), (*ok, dict(offsets=torch.zeros(3, **i32), rows=4)),
+                              (torch.zeros(384, 32, **u8), torch.zeros(3, 1, 512, **u8), dict(offsets=torch.zeros(3), rows=4))):
+        with pytest.raises(ValueError):
+            binding.Mx4(codes, scales, **kw)
+    x = torch.zeros(4, 64, device="cuda")
+    for bad in (dict(x=x[:, :40]), dict(x=x.half()), dict(x=x.cpu()), dict(x=x.t()), dict(offsets=torch.zeros(3, device="cuda")), dict(slot_of_row=torch.zeros(3, device="cuda"))):
+        with pytest.raises(ValueError):
+            binding.mx4_quantize(**{"x": x, **bad})
+    q, w = binding.mx4_quantize(x), binding.Mx4(torch.zeros(8, 32, **u8), torch.zeros(1, 1, 512, **u8))
+    with pytest.raises(ValueError):
+        binding.mx4_matmul(q, w, out=torch.empty(4, 9, device="cuda"))
+    with pytest.raises(ValueError):
+        binding.mx4_matmul(q, w, dtype=torch.float16)
+    with pytest.raises(ValueError):
+        binding.mx4_matmul_mx4(q, w)                                     # eight columns are no block
+    with pytest.raises(binding.BigmacError):
+        binding.mx4_matmul(q, binding.mx4_quantize(torch.zeros(8, 32, device="cuda")))

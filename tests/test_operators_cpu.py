@@ -97,10 +97,11 @@ def test_binding_refuses_what_is_no_4_bit_matrix():
                               (torch.zeros(4, 32, dtype=u8), torch.zeros(1, 2, 512, dtype=u8), {}),
                               (torch.zeros(129, 32, dtype=u8), torch.zeros(1, 1, 512, dtype=u8), {}),
                               (torch.zeros(2, 4, 32, dtype=u8), torch.zeros(1, 1, 512, dtype=u8), {}),
+                              (torch.zeros(4, 32, dtype=u8), torch.zeros(1, 1, 512, dtype=u8), {}),                            # not on a GPU
                               (torch.zeros(4, 32, dtype=u8), torch.zeros(1, 1, 512, dtype=u8), dict(offsets=torch.zeros(3, dtype=torch.int32))),
                               (torch.zeros(4, 32, dtype=u8), torch.zeros(1, 1, 512, dtype=u8), dict(offsets=torch.zeros(3, dtype=torch.int32), rows=4))):
         with pytest.raises(ValueError):
-            binding._mx4(binding.Mx4(codes, scales, **kw), -1)
+            binding.Mx4(codes, scales, **kw)
     with pytest.raises(ValueError):
         binding._dtype(torch.float16)
 
