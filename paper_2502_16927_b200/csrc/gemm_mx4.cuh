@@ -53,15 +53,15 @@ __host__ __device__ constexpr uint32_t instr_desc_mx4(int bn, int half) {
            ((uint32_t)(2 * half) << 29);
 }
 
-// GELU of 32 accumulators for an output in bf16: z Phi(z), Phi(z) = sat(1/2 + z P(z^2)).  P is the minimax fit in the error of z Phi(z) on
-// |z| <= 4.5 (reweighted least squares on Chebyshev nodes), of even degree with a positive leading coefficient, so that behind 4.5 the
-// saturating multiply-add holds Phi at 0 or 1 without a look at the argument.  z Phi(z) is off by less than 3e-6 up to 4.5 and by less
-// than 3.3e-5 everywhere (at -4.5, where it is -1.5e-5 itself): a bf16 step of 1/2 is 4e-3.  Seven instructions an element; a form that
-// keeps the relative precision of the negative tail (a polynomial times an exponential) took twelve and, at 131072 rows of r 256, h 1024,
-// 96 us, erff 142.
+// GELU of 32 accumulators for an output in bf16 or 4 bits: z Phi(z), Phi(z) = sat(1/2 + z P(z^2)).  P is the minimax fit in the error of z Phi(z) on
+// |z| <= 4.3 (reweighted least squares on Chebyshev nodes), of even degree with a positive leading coefficient, so that behind 4.3 the
+// saturating multiply-add holds Phi at 0 or 1 without a look at the argument.  z Phi(z) is off by less than 2e-5 up to 4.3 and by less
+// than 3.6e-5 everywhere (at 4.3); a bf16 step of 1/2 is 4e-3.  The FMA pipe bounds this epilogue: eleven multiply-adds an element, 1408 cycles a
+// tile of 128 x 128.  131072 rows of r 256, h 1024: 78 us, with degree 10 (1.4e-6 up to 4.5) 85, without an activation 54; a polynomial times an
+// exponential, which keeps the relative precision of the negative tail, 96; erff 142.
 __device__ __forceinline__ void gelu_chunk(float* v) {
-    constexpr float kC[11] = {0.3989286422729492f, -0.06644835323095322f, 0.009928264655172825f, -0.0011627154890447855f, 0.00010752371599664912f, -7.800386811140925e-06f,
-                              4.3196823185098765e-07f, -1.7442022937075308e-08f, 4.790651764174925e-10f, -7.938010491981284e-12f, 5.954283154854453e-14f};
+    constexpr float kC[9] = {0.3988020718097687f, -0.06615559756755829f, 0.009695150889456272f, -0.0010713869705796242f, 8.711775444680825e-05f,
+                             -5.0061771617038175e-06f, 1.9022436958948674e-07f, -4.249006924084142e-09f, 4.197454883669849e-11f};
     constexpr int kG = 8;                                  // pairs side by side, so that no multiply-add waits for the one before
 #pragma unroll
     for (int g = 0; g < 16; g += kG) {
@@ -70,10 +70,10 @@ __device__ __forceinline__ void gelu_chunk(float* v) {
         for (int i = 0; i < kG; ++i) {
             const f32x2_t z = pk2(v[2 * (g + i)], v[2 * (g + i) + 1]);
             w[i] = mul2(z, z);
-            P[i] = fma2(pk2(kC[10], kC[10]), w[i], pk2(kC[9], kC[9]));
+            P[i] = fma2(pk2(kC[8], kC[8]), w[i], pk2(kC[7], kC[7]));
         }
 #pragma unroll
-        for (int k = 8; k >= 0; --k)
+        for (int k = 6; k >= 0; --k)
 #pragma unroll
             for (int i = 0; i < kG; ++i) P[i] = fma2(P[i], w[i], pk2(kC[k], kC[k]));
 #pragma unroll

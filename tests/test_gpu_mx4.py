@@ -108,9 +108,9 @@ def _check_product(got, a, w, act, dtype):
     K = a.shape[1]
     want = _act(z, act)
     err = 1.13 * (K / 64 + 2) * 2.0 ** -23 * S + (np.abs(z) * 2.0 ** -20 if act in (1, 2) else 0)
-    # GELU of a bf16 output is a polynomial under saturation, off by less than 3.3e-5: its minimax error and its fp32 evaluation, looked at on
-    # two million points of [-12, 12]; outside Phi is 0 or 1 and so is the polynomial's sum
-    err += 3.3e-5 if act == 1 and dtype == torch.bfloat16 else 0
+    # GELU of a bf16 output is a polynomial under saturation, off by less than 3.6e-5: its minimax error and its fp32 evaluation, looked at on
+    # four million points of [-40, 40]; outside Phi is 0 or 1 and so is the polynomial's sum
+    err += 3.6e-5 if act == 1 and dtype == torch.bfloat16 else 0
     err += np.abs(want) * torch.finfo(dtype).eps / 2 * 1.01
     diff = np.abs(got.double().cpu().numpy() - want)
     assert (diff <= err).all(), (float((diff - err).max()), float((diff / np.maximum(np.abs(want), 1e-30)).max()))
@@ -267,7 +267,7 @@ def test_product_in_4_bits(binding, E, rows, N, K, act):
         z = a[seg] @ w[e].T
         want = _act(z, act)
         S = np.abs(a[seg]) @ np.abs(w[e]).T
-        err = 1.13 * (K / 64 + 2) * 2.0 ** -23 * S + (3.3e-5 if act == 1 else np.abs(z) * 2.0 ** -20)     # as for a product in bf16, without its rounding
+        err = 1.13 * (K / 64 + 2) * 2.0 ** -23 * S + (3.6e-5 if act == 1 else np.abs(z) * 2.0 ** -20)     # as for a product in bf16, without its rounding
         blocks, slack = want.reshape(-1, N // 32, 32), err.reshape(-1, N // 32, 32)
         top = np.abs(blocks).max(-1, keepdims=True)
         ok = np.zeros(blocks.shape, dtype=bool)
