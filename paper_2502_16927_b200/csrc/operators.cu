@@ -47,7 +47,7 @@ Mx4View view_of(const bigmac_mx4_t* q) {
 // A matrix of the joint: aligned to its elements, rows that do not overlap.  *vec: rows on 16-byte boundaries, too.
 bool rows_ok(const bigmac_rows_t& m, int64_t d, int64_t es, bool* vec) {
     if (!m.p) return true;
-    if (!is_aligned(m.p, es) || m.ld < d) return false;
+    if (!is_aligned(m.p, es) || m.ld < d || m.ld > 0x7fffffff) return false;
     if (!is_aligned(m.p, 16) || (m.ld * es) % 16) *vec = false;
     return true;
 }
@@ -63,7 +63,7 @@ int check_residual_norm(const bigmac_residual_norm_t* q, int32_t T, bool backwar
         return BIGMAC_ERR_INVALID_ARG;
     if (!(q->post_eps >= 0) || !(q->pre_eps >= 0) || !std::isfinite(q->post_eps) || !std::isfinite(q->pre_eps) || !std::isfinite(q->residual_scale))
         return BIGMAC_ERR_INVALID_ARG;
-    if (q->d > kResNormMaxWidth) return BIGMAC_ERR_UNSUPPORTED;
+    if (q->d > kResNormMaxWidth || T > kResNormMaxRows) return BIGMAC_ERR_UNSUPPORTED;
     const int64_t es = esize_of(q->dtype);
     *a = ResNorm{q, T, q->d % 8 == 0};
     bool ok = rows_ok(q->x, q->d, es, &a->vec) && rows_ok(q->y, q->d, es, &a->vec) && vector_ok(q->w_post, &a->vec) && vector_ok(q->b_post, &a->vec) &&

@@ -29,20 +29,20 @@ __global__ void __launch_bounds__(1024 / NV) residual_norm_kernel(const Params p
     const int in_block = threads == 32 ? threadIdx.x >> 5 : 0;
     Row at{sums[0], sums[1], threads == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads, 1};
     const int t = at.t;
-    const int64_t row = (int64_t)blockIdx.x * (threads == 32 ? blockDim.x >> 5 : 1) + in_block;
+    const int row = (int)blockIdx.x * (threads == 32 ? (int)blockDim.x >> 5 : 1) + in_block;
     if (row >= p.T) return;
     f2 r[4 * NV], y[4 * NV];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) load8<T, VEC>((const T*)p.x + row * p.x_ld, v, t, threads, p.d, r + 4 * v);
+    for (int v = 0; v < NV; ++v) load8<T, VEC>(row_at((const T*)p.x, row, p.x_ld), v, t, threads, p.d, r + 4 * v);
     float4 st = make_float4(0.0f, 1.0f, 0.0f, 1.0f);
     const f2 rho = pk(p.rho);
     if (p.y) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) load8<T, VEC>((const T*)p.y + row * p.y_ld, v, t, threads, p.d, y + 4 * v);
+        for (int v = 0; v < NV; ++v) load8<T, VEC>(row_at((const T*)p.y, row, p.y_ld), v, t, threads, p.d, y + 4 * v);
         f2 g[4 * NV];
         if (p.gate_kind == BIGMAC_GATE_FULL) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) load8<T, VEC>((const T*)p.gate + row * p.gate_ld, v, t, threads, p.d, g + 4 * v);
+            for (int v = 0; v < NV; ++v) load8<T, VEC>(row_at((const T*)p.gate, row, p.gate_ld), v, t, threads, p.d, g + 4 * v);
         } else if (p.gate_kind == BIGMAC_GATE_CHANNEL) {
 #pragma unroll
             for (int v = 0; v < NV; ++v) load8<float, VEC>((const float*)p.gate, v, t, threads, p.d, g + 4 * v);
@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(1024 / NV) residual_norm_kernel(const Params p
     }
     if (p.r) {
 #pragma unroll
-        for (int v = 0; v < NV; ++v) store8<T, VEC>((T*)p.r + row * p.r_ld, v, t, threads, p.d, r + 4 * v);
+        for (int v = 0; v < NV; ++v) store8<T, VEC>(row_at((T*)p.r, row, p.r_ld), v, t, threads, p.d, r + 4 * v);
     }
     if (p.n) {
         row_stats<NV, VEC>(p.pre, r, p.pre_eps, p, at, st.z, st.w);
@@ -82,7 +82,7 @@ __global__ void __launch_bounds__(1024 / NV) residual_norm_kernel(const Params p
             param8<VEC>(p.b_pre, 0.0f, v, t, threads, p.d, b);
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = fma2(mul2(add2(r[4 * v + j], pk(-st.z)), pk(st.w)), w[j], b[j]);
-            store8<T, VEC>((T*)p.n + row * p.n_ld, v, t, threads, p.d, w);
+            store8<T, VEC>(row_at((T*)p.n, row, p.n_ld), v, t, threads, p.d, w);
         }
     }
     if (p.stats && t == 0) p.stats[row] = st;
@@ -100,11 +100,11 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
     grid_dependency_wait();
     const int t = threadIdx.x % threads, group = threadIdx.x / threads, groups = kThreads / threads;
     if (group >= groups) return;                                       // threads that are no whole row
-    const int64_t first = (int64_t)blockIdx.x * groups + group, step = (int64_t)gridDim.x * groups;
+    const int first = (int)blockIdx.x * groups + group, step = (int)gridDim.x * groups;
     Row at{sums[0][group], sums[1][group], t, threads, 1 + group};
     Ring<T, VEC, COUNT> ring;
     const void* const in[3] = {p.x, p.y, p.gate};
-    const int64_t ld[3] = {p.x_ld, p.y_ld, p.gate_ld};
+    const int ld[3] = {p.x_ld, p.y_ld, p.gate_ld};
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) { ring.in[i] = (const T*)in[i]; ring.ld[i] = ld[i]; ring.has[i] = true; }
     ring.init(smem + vectors * kParamBytes, group, stages, p);
@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
     }
     int stage = 0;
     const f2 rho = pk(p.rho);
-    for (int64_t row = first; row < p.T; row += step) {
+    for (int row = first; row < p.T; row += step) {
         const float token = GATE == BIGMAC_GATE_TOKEN ? ((const float*)p.gate)[row] : 1.0f;
         ring.next(stage, row, step, at);
         f2 r[4];
@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
             }
             cut8<VEC>(0, t, threads, p.d, r);
         }
-        if (p.r) store8<T, VEC>((T*)p.r + row * p.r_ld, 0, t, threads, p.d, r);
+        if (p.r) store8<T, VEC>(row_at((T*)p.r, row, p.r_ld), 0, t, threads, p.d, r);
         if (p.n) {
             f2 w[4], b[4];
             row_stats<1, VEC>(p.pre, r, p.pre_eps, p, at, st.z, st.w);
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
             if (vectors == 4) par.get(3, b); else fill8(0.0f, b);
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = fma2(mul2(add2(r[j], pk(-st.z)), pk(st.w)), w[j], b[j]);
-            store8<T, VEC>((T*)p.n + row * p.n_ld, 0, t, threads, p.d, w);
+            store8<T, VEC>(row_at((T*)p.n, row, p.n_ld), 0, t, threads, p.d, w);
         }
         if (p.stats && t == 0) p.stats[row] = st;
         stage = stage + 1 == stages ? 0 : stage + 1;
@@ -218,8 +218,8 @@ Params resnorm::params_of(const ResNorm& a) {
     Params p{};
     p.x = q.x.p; p.y = q.y.p; p.gate = q.gate.p; p.dr = q.dr.p; p.dn = q.dn.p;
     p.r = q.r.p; p.n = q.n.p; p.dx = q.dx.p; p.dy = q.dy.p; p.dgate = q.dgate.p;
-    p.x_ld = q.x.ld; p.y_ld = q.y.ld; p.gate_ld = q.gate.ld; p.dr_ld = q.dr.ld; p.dn_ld = q.dn.ld;
-    p.r_ld = q.r.ld; p.n_ld = q.n.ld; p.dx_ld = q.dx.ld; p.dy_ld = q.dy.ld; p.dgate_ld = q.dgate.ld;
+    p.x_ld = (int)q.x.ld; p.y_ld = (int)q.y.ld; p.gate_ld = (int)q.gate.ld; p.dr_ld = (int)q.dr.ld; p.dn_ld = (int)q.dn.ld;
+    p.r_ld = (int)q.r.ld; p.n_ld = (int)q.n.ld; p.dx_ld = (int)q.dx.ld; p.dy_ld = (int)q.dy.ld; p.dgate_ld = (int)q.dgate.ld;
     p.w_post = q.w_post; p.b_post = q.b_post; p.w_pre = q.w_pre; p.b_pre = q.b_pre;
     p.stats = (float4*)q.stats;
     p.rho = q.residual_scale; p.post_eps = q.post_eps; p.pre_eps = q.pre_eps; p.inv_d = 1.0f / (float)q.d;

@@ -8,10 +8,14 @@ namespace resnorm {
 
 constexpr unsigned kAll = 0xffffffffu;
 
+// Row `row` of a matrix.
+template <typename T>
+__device__ __forceinline__ T* row_at(T* p, int row, int ld) { return p + (int64_t)row * ld; }
+
 struct Params {
     const void *x, *y, *gate, *dr, *dn;
     void *r, *n, *dx, *dy, *dgate;
-    int64_t x_ld, y_ld, gate_ld, dr_ld, dn_ld, r_ld, n_ld, dx_ld, dy_ld, dgate_ld;
+    int x_ld, y_ld, gate_ld, dr_ld, dn_ld, r_ld, n_ld, dx_ld, dy_ld, dgate_ld;      // 32 bits: a row's place is one wide multiplication
     const float *w_post, *b_post, *w_pre, *b_pre;
     float4* stats;
     float* partial;
@@ -226,7 +230,7 @@ template <typename T, bool VEC, int COUNT>
 struct Ring {
     static constexpr int kHalves = (int)sizeof(T) / 2;
     const T* in[COUNT];
-    int64_t ld[COUNT];
+    int ld[COUNT];
     bool has[COUNT];
     uint8_t* base;                                                     // VEC: the thread's first slot; else the group's
     int stages, T_rows, d;
@@ -241,8 +245,8 @@ struct Ring {
         return base + (VEC ? (uint32_t)(stage * COUNT + which) * kHalves * kPieceBytes : (uint32_t)(stage * COUNT + which) * granules);
     }
     // Fewer than 16 bytes of the tensor before or behind the row.
-    __device__ __forceinline__ bool direct(int64_t row) const { return !VEC && (row * d < 16 || (T_rows - 1 - row) * d < 16); }
-    __device__ __forceinline__ void fetch(int stage, int64_t row, int t, int threads) {
+    __device__ __forceinline__ bool direct(int row) const { return !VEC && ((int64_t)row * d < 16 || (int64_t)(T_rows - 1 - row) * d < 16); }
+    __device__ __forceinline__ void fetch(int stage, int row, int t, int threads) {
         if (row < T_rows && !direct(row)) {
             if constexpr (VEC) {
                 const int c = t * 8;
@@ -250,7 +254,7 @@ struct Ring {
 #pragma unroll
                     for (int i = 0; i < COUNT; ++i) {
                         if (!has[i]) continue;
-                        const T* from = in[i] + row * ld[i] + c;
+                        const T* from = row_at(in[i], row, ld[i]) + c;
                         const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot(stage, i));
 #pragma unroll
                         for (int h = 0; h < kHalves; ++h) copy16(to + h * kPieceBytes, from + h * 4);
@@ -260,7 +264,7 @@ struct Ring {
 #pragma unroll
                 for (int i = 0; i < COUNT; ++i) {
                     if (!has[i]) continue;
-                    const uintptr_t from = (uintptr_t)(in[i] + row * ld[i]);
+                    const uintptr_t from = (uintptr_t)row_at(in[i], row, ld[i]);
                     const uint8_t* first = (const uint8_t*)(from & ~(uintptr_t)15);
                     const uint32_t bytes = (uint32_t)(from & 15) + d * (uint32_t)sizeof(T);
                     const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot(stage, i));
@@ -271,11 +275,11 @@ struct Ring {
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
     // Rows first, first + step, ... up to the (stages - 1)-th are asked for.
-    __device__ __forceinline__ void start(int64_t first, int64_t step, int t, int threads) {
+    __device__ __forceinline__ void start(int first, int step, int t, int threads) {
         for (int s = 0; s < stages - 1; ++s) fetch(s, first + s * step, t, threads);
     }
     // Row `row` is in its stage, the one stages - 1 rows later on its way.
-    __device__ __forceinline__ void next(int stage, int64_t row, int64_t step, const Row& at) {
+    __device__ __forceinline__ void next(int stage, int row, int step, const Row& at) {
         if constexpr (VEC) {
             fetch(stage == 0 ? stages - 1 : stage - 1, row + (stages - 1) * step, at.t, at.threads);
             wait_groups(stages - 1);
@@ -293,7 +297,7 @@ struct Ring {
         if (at.threads == 32) __syncwarp();
         else row_barrier(at.id, at.threads);
     }
-    __device__ __forceinline__ void get(int stage, int which, int64_t row, int t, int threads, f2* f) const {
+    __device__ __forceinline__ void get(int stage, int which, int row, int t, int threads, f2* f) const {
         if (!has[which]) { fill8(0.0f, f); return; }
         if constexpr (VEC) {
             if (t * 8 < d) {
@@ -308,7 +312,7 @@ struct Ring {
                 fill8(0.0f, f);
             }
         } else {
-            const T* from = in[which] + row * ld[which];
+            const T* from = row_at(in[which], row, ld[which]);
             load8<T, false>(direct(row) ? from : (const T*)(slot(stage, which) + ((uintptr_t)from & 15)), 0, t, threads, d, f);
         }
     }

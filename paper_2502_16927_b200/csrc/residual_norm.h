@@ -5,6 +5,7 @@
 namespace bigmac {
 
 constexpr int kResNormMaxWidth = 8192;
+constexpr int kResNormMaxRows = 1 << 30;    // row numbers and the step behind the last one are 32-bit
 
 struct ResNorm {
     const bigmac_residual_norm_t* q;

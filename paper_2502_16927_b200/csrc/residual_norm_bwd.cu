@@ -25,7 +25,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Pa
     grid_dependency_launch();
     grid_dependency_wait();
     const int t = threadIdx.x % threads, group = threadIdx.x / threads, groups = kThreads / threads;
-    const int64_t first = (int64_t)blockIdx.x * groups + group, step = (int64_t)gridDim.x * groups;
+    const int first = (int)blockIdx.x * groups + group, step = (int)gridDim.x * groups;
     const bool working = group < groups;                               // threads that are no whole row rest
     Row at{sums[0][working ? group : 0], sums[1][working ? group : 0], t, threads, 1 + group};
     const int gate_kind = GATE == kAnyGate ? p.gate_kind : GATE;       // RING: a channel gate counts as none
@@ -35,9 +35,9 @@ __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Pa
     ring.in[IN_X] = (const T*)p.x; ring.in[IN_Y] = (const T*)p.y; ring.in[IN_DR] = (const T*)p.dr; ring.in[IN_DN] = (const T*)p.dn; ring.in[IN_GATE] = (const T*)p.gate;
     ring.ld[IN_X] = p.x_ld; ring.ld[IN_Y] = p.y_ld; ring.ld[IN_DR] = p.dr_ld; ring.ld[IN_DN] = p.dn_ld; ring.ld[IN_GATE] = p.gate_ld;
     ring.has[IN_X] = true; ring.has[IN_Y] = has_y; ring.has[IN_DR] = p.dr != nullptr; ring.has[IN_DN] = has_dn; ring.has[IN_GATE] = gate_kind == BIGMAC_GATE_FULL;
-    auto get = [&](int stage, int which, int v, int64_t row, f2* f) {
+    auto get = [&](int stage, int which, int v, int row, f2* f) {
         if constexpr (RING) ring.get(stage, which, row, t, threads, f);
-        else if (ring.has[which]) load8<T, VEC>(ring.in[which] + row * ring.ld[which], v, t, threads, p.d, f);
+        else if (ring.has[which]) load8<T, VEC>(row_at(ring.in[which], row, ring.ld[which]), v, t, threads, p.d, f);
         else fill8(0.0f, f);
     };
     ParamStore par{smem + threadIdx.x * 16};                           // RING: w_post, b_post, w_pre
@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Pa
         int stage = 0;
         const f2 rho = pk(p.rho);
         float4 next_stats = first < p.T ? p.stats[first] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        for (int64_t row = first; row < p.T; row += step) {
+        for (int row = first; row < p.T; row += step) {
             const float4 st = next_stats;
             if (row + step < p.T) next_stats = p.stats[row + step];
             const float token = gate_kind == BIGMAC_GATE_TOKEN ? ((const float*)p.gate)[row] : 1.0f;
@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Pa
                     f2 o[4];
 #pragma unroll
                     for (int j = 0; j < 4; ++j) o[j] = mul2(rho, D[4 * v + j]);
-                    store8<T, VEC>((T*)p.dx + row * p.dx_ld, v, t, threads, p.d, o);
+                    store8<T, VEC>(row_at((T*)p.dx, row, p.dx_ld), v, t, threads, p.d, o);
                 }
             }
             if (has_y) {
@@ -137,7 +137,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Pa
                         f2 o[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) o[j] = mul2(D[4 * v + j], a[4 * v + j]);
-                        store8<T, VEC>((T*)p.dgate + row * p.dgate_ld, v, t, threads, p.d, o);
+                        store8<T, VEC>(row_at((T*)p.dgate, row, p.dgate_ld), v, t, threads, p.d, o);
                     }
                 }
                 // sums of p and p hat; a channel gate's factor joins the column sums at the end
@@ -173,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Pa
                         for (int i = 0; i < 4 * NV; ++i) D[i] = mul2(pk(st.y), fma2(hat[i], pk(m1), add2(D[i], pk(m0))));
                     }
 #pragma unroll
-                    for (int v = 0; v < NV; ++v) store8<T, VEC>((T*)p.dy + row * p.dy_ld, v, t, threads, p.d, D + 4 * v);
+                    for (int v = 0; v < NV; ++v) store8<T, VEC>(row_at((T*)p.dy, row, p.dy_ld), v, t, threads, p.d, D + 4 * v);
                 }
             }
             if constexpr (RING) stage = stage + 1 == stages ? 0 : stage + 1;
