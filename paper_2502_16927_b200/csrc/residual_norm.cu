@@ -107,23 +107,23 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
     const int ld[3] = {p.x_ld, p.y_ld, p.gate_ld};
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) { ring.in[i] = (const T*)in[i]; ring.ld[i] = ld[i]; ring.has[i] = true; }
-    ring.init(smem + vectors * kParamBytes, group, stages, p);
+    ring.init(smem + vectors * param_bytes(false, threads, 1), group, stages, p);
     ring.start(first, step, t, threads);
-    // vectors 0, 1: w and b of the norm before, 2, 3: of the one behind; b only with `vectors` = 4
-    ParamStore par{smem + threadIdx.x * 16};
+    // vectors 0, 1: w and b of the norm before, 2, 3: of the one behind; b only with `vectors` = 4.
+    ParamStore<1, false> par(smem, t, threads);
     const int pre = vectors / 2;
     {
         f2 w[4], b[4];
         if (GATE != kNoBlock) {
-            post_params<VEC>(p, t, threads, w, b);
-            par.put(0, w);
-            if (vectors == 4) par.put(1, b);
+            post_params<VEC>(p, 0, t, threads, w, b);
+            par.put(0, 0, w);
+            if (vectors == 4) par.put(1, 0, b);
         }
         param8<VEC>(p.w_pre, 1.0f, 0, t, threads, p.d, w);
-        par.put(pre, w);
+        par.put(pre, 0, w);
         if (vectors == 4) {
             param8<VEC>(p.b_pre, 0.0f, 0, t, threads, p.d, b);
-            par.put(3, b);
+            par.put(3, 0, b);
         }
     }
     int stage = 0;
@@ -133,16 +133,16 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
         ring.next(stage, row, step, at);
         f2 r[4];
         float4 st = make_float4(0.0f, 1.0f, 0.0f, 1.0f);
-        ring.get(stage, 0, row, t, threads, r);
+        ring.get(stage, 0, 0, row, t, threads, r);
 #pragma unroll
         for (int j = 0; j < 4; ++j) r[j] = mul2(rho, r[j]);
         if constexpr (GATE != kNoBlock) {
             f2 y[4], w[4], b[4], g[4];
-            ring.get(stage, 1, row, t, threads, y);
-            if constexpr (GATE == BIGMAC_GATE_FULL) ring.get(stage, 2, row, t, threads, g);
+            ring.get(stage, 1, 0, row, t, threads, y);
+            if constexpr (GATE == BIGMAC_GATE_FULL) ring.get(stage, 2, 0, row, t, threads, g);
             row_stats<1, VEC>(p.post, y, p.post_eps, p, at, st.x, st.y);
-            par.get(0, w);
-            if (vectors == 4) par.get(1, b); else fill8(0.0f, b);
+            par.get(0, 0, w);
+            if (vectors == 4) par.get(1, 0, b); else fill8(0.0f, b);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const f2 a = fma2(mul2(add2(y[j], pk(-st.x)), pk(st.y)), w[j], b[j]);
@@ -154,8 +154,8 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
         if (p.n) {
             f2 w[4], b[4];
             row_stats<1, VEC>(p.pre, r, p.pre_eps, p, at, st.z, st.w);
-            par.get(pre, w);
-            if (vectors == 4) par.get(3, b); else fill8(0.0f, b);
+            par.get(pre, 0, w);
+            if (vectors == 4) par.get(3, 0, b); else fill8(0.0f, b);
 #pragma unroll
             for (int j = 0; j < 4; ++j) w[j] = fma2(mul2(add2(r[j], pk(-st.z)), pk(st.w)), w[j], b[j]);
             store8<T, VEC>(row_at((T*)p.n, row, p.n_ld), 0, t, threads, p.d, w);
@@ -180,7 +180,7 @@ cudaError_t persistent(const ResNorm& a, cudaStream_t stream) {
     auto kernel = residual_norm_rows_kernel<T, VEC, GATE>;
     const int threads = threads_of(a.q->d, 1), groups = kThreads / threads, count = GATE == kNoBlock ? 1 : GATE == BIGMAC_GATE_FULL ? 3 : 2;
     const int vectors = a.q->b_post || a.q->b_pre ? 4 : 2;
-    const size_t stage = stage_bytes(VEC, a.q->d, (int)sizeof(T), groups, count), left = kRowsSmem - vectors * kParamBytes;
+    const size_t stage = stage_bytes(VEC, a.q->d, (int)sizeof(T), groups, count), par = vectors * param_bytes(false, threads, 1), left = kRowsSmem - par;
     const int stages = (int)(left / stage < 1 ? 1 : left / stage > 4 ? 4 : left / stage);
     static PerDeviceOnce once;
     int dev;
@@ -190,7 +190,7 @@ cudaError_t persistent(const ResNorm& a, cudaStream_t stream) {
         once.mark(dev);
     }
     const int64_t want = ((int64_t)a.T + groups - 1) / groups, most = 2 * (int64_t)gemm_tc_sm_count();
-    return launch_chained(kernel, (int)(want < most ? want : most), kThreads, vectors * kParamBytes + stages * stage, stream, params_of(a), threads, stages, vectors);
+    return launch_chained(kernel, (int)(want < most ? want : most), kThreads, par + stages * stage, stream, params_of(a), threads, stages, vectors);
 }
 template <typename T, bool VEC>
 cudaError_t persistent_by_gate(const ResNorm& a, cudaStream_t stream) {

@@ -218,17 +218,17 @@ __device__ __forceinline__ void wait_groups(int pending) {
 // Bytes of one tensor's row in a stage where rows lie at any address: the 16-byte granules that it touches.
 __host__ __device__ inline uint32_t granule_bytes(int d, int es) { return (uint32_t)(d * es / 16 + 2) * 16; }
 // Bytes of a stage of a block whose rows have `count` tensors.
-inline size_t stage_bytes(bool vec, int d, int es, int groups, int count) {
-    return vec ? (size_t)count * (es / 2) * kPieceBytes : (size_t)count * groups * granule_bytes(d, es);
+inline size_t stage_bytes(bool vec, int d, int es, int groups, int count, int nv = 1) {
+    return vec ? (size_t)count * nv * (es / 2) * kPieceBytes : (size_t)count * groups * granule_bytes(d, es);
 }
 
 // The rows a group of threads works on, `stages` of them in shared memory or on their way there.
 // VEC: every thread copies and reads its own 16 bytes, so no thread waits for another.  Else a row begins anywhere: its threads copy the 16-byte
 // granules that hold it and read single elements after a barrier; the first and the last rows of all, whose granules may reach out of the
 // tensor, are read directly.
-template <typename T, bool VEC, int COUNT>
+template <typename T, bool VEC, int COUNT, int NV = 1>
 struct Ring {
-    static constexpr int kHalves = (int)sizeof(T) / 2;
+    static constexpr int kHalves = (int)sizeof(T) / 2;                 // 16-byte pieces of eight elements
     const T* in[COUNT];
     int ld[COUNT];
     bool has[COUNT];
@@ -242,22 +242,24 @@ struct Ring {
         base = VEC ? smem + threadIdx.x * 16 : smem + (size_t)group * stages * COUNT * granules;
     }
     __device__ __forceinline__ uint8_t* slot(int stage, int which) const {
-        return base + (VEC ? (uint32_t)(stage * COUNT + which) * kHalves * kPieceBytes : (uint32_t)(stage * COUNT + which) * granules);
+        return base + (VEC ? (uint32_t)(stage * COUNT + which) * NV * kHalves * kPieceBytes : (uint32_t)(stage * COUNT + which) * granules);
     }
     // Fewer than 16 bytes of the tensor before or behind the row.
     __device__ __forceinline__ bool direct(int row) const { return !VEC && ((int64_t)row * d < 16 || (int64_t)(T_rows - 1 - row) * d < 16); }
     __device__ __forceinline__ void fetch(int stage, int row, int t, int threads) {
         if (row < T_rows && !direct(row)) {
             if constexpr (VEC) {
-                const int c = t * 8;
-                if (c < d) {
 #pragma unroll
-                    for (int i = 0; i < COUNT; ++i) {
-                        if (!has[i]) continue;
-                        const T* from = row_at(in[i], row, ld[i]) + c;
-                        const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot(stage, i));
+                for (int i = 0; i < COUNT; ++i) {
+                    if (!has[i]) continue;
+                    const T* from = row_at(in[i], row, ld[i]);
+                    const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot(stage, i));
 #pragma unroll
-                        for (int h = 0; h < kHalves; ++h) copy16(to + h * kPieceBytes, from + h * 4);
+                    for (int v = 0; v < NV; ++v) {
+                        const int c = column<true>(v, 0, t, threads);
+                        if (c >= d) continue;
+#pragma unroll
+                        for (int h = 0; h < kHalves; ++h) copy16(to + (v * kHalves + h) * kPieceBytes, from + c + h * 4);
                     }
                 }
             } else {
@@ -297,11 +299,12 @@ struct Ring {
         if (at.threads == 32) __syncwarp();
         else row_barrier(at.id, at.threads);
     }
-    __device__ __forceinline__ void get(int stage, int which, int row, int t, int threads, f2* f) const {
+    // Piece v of a row.
+    __device__ __forceinline__ void get(int stage, int which, int v, int row, int t, int threads, f2* f) const {
         if (!has[which]) { fill8(0.0f, f); return; }
         if constexpr (VEC) {
-            if (t * 8 < d) {
-                const uint8_t* s = slot(stage, which);
+            if (column<true>(v, 0, t, threads) < d) {
+                const uint8_t* s = slot(stage, which) + v * kHalves * kPieceBytes;
                 if constexpr (sizeof(T) == 2) {
                     unpack8(*(const uint4*)s, f);
                 } else {
@@ -313,32 +316,39 @@ struct Ring {
             }
         } else {
             const T* from = row_at(in[which], row, ld[which]);
-            load8<T, false>(direct(row) ? from : (const T*)(slot(stage, which) + ((uintptr_t)from & 15)), 0, t, threads, d, f);
+            load8<T, false>(direct(row) ? from : (const T*)(slot(stage, which) + ((uintptr_t)from & 15)), v, t, threads, d, f);
         }
     }
 };
 
-// Vectors of parameters in shared memory, every thread its own columns: vector `which`, 32 bytes in two pieces.
+// Vectors of parameters in shared memory: piece v of vector `which`, 32 bytes in two pieces.  Every thread its own columns, which takes constant
+// offsets (7 % of the forward); SHARED: the rows of a block read the same ones, where there is no room for that.
+template <int NV, bool SHARED>
 struct ParamStore {
     uint8_t* base;                                                     // the thread's first piece
-    __device__ __forceinline__ void put(int which, const f2* f) {
-        *(ulonglong2*)(base + (2 * which) * kPieceBytes) = make_ulonglong2(f[0], f[1]);
-        *(ulonglong2*)(base + (2 * which + 1) * kPieceBytes) = make_ulonglong2(f[2], f[3]);
+    uint32_t row_step;                                                 // SHARED: from piece to piece, 16 bytes of every thread of a row
+    __device__ __forceinline__ ParamStore(uint8_t* smem, int t, int threads) : base(smem + (SHARED ? t : (int)threadIdx.x) * 16), row_step(threads * 16) {}
+    __device__ __forceinline__ uint32_t step() const { return SHARED ? row_step : kPieceBytes; }
+    __device__ __forceinline__ uint8_t* at(int which, int v) const { return base + (uint32_t)(2 * (which * NV + v)) * step(); }
+    __device__ __forceinline__ void put(int which, int v, const f2* f) {
+        *(ulonglong2*)at(which, v) = make_ulonglong2(f[0], f[1]);
+        *(ulonglong2*)(at(which, v) + step()) = make_ulonglong2(f[2], f[3]);
     }
-    __device__ __forceinline__ void get(int which, f2* f) const {
-        const ulonglong2 a = *(const ulonglong2*)(base + (2 * which) * kPieceBytes), b = *(const ulonglong2*)(base + (2 * which + 1) * kPieceBytes);
+    __device__ __forceinline__ void get(int which, int v, f2* f) const {
+        const ulonglong2 a = *(const ulonglong2*)at(which, v), b = *(const ulonglong2*)(at(which, v) + step());
         f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
     }
 };
-constexpr uint32_t kParamBytes = 2 * kPieceBytes;                      // of one vector
+// Bytes of one vector.
+__host__ __device__ inline uint32_t param_bytes(bool shared, int threads, int nv) { return (uint32_t)(shared ? threads : kThreads) * nv * 32; }
 // w_post and b_post, a channel gate multiplied in (gate (hat w + b) = hat (gate w) + gate b).
 template <bool VEC>
-__device__ __forceinline__ void post_params(const Params& p, int t, int threads, f2* w, f2* b) {
-    param8<VEC>(p.w_post, 1.0f, 0, t, threads, p.d, w);
-    param8<VEC>(p.b_post, 0.0f, 0, t, threads, p.d, b);
+__device__ __forceinline__ void post_params(const Params& p, int v, int t, int threads, f2* w, f2* b) {
+    param8<VEC>(p.w_post, 1.0f, v, t, threads, p.d, w);
+    param8<VEC>(p.b_post, 0.0f, v, t, threads, p.d, b);
     if (p.gate_kind == BIGMAC_GATE_CHANNEL) {
         f2 g[4];
-        load8<float, VEC>((const float*)p.gate, 0, t, threads, p.d, g);
+        load8<float, VEC>((const float*)p.gate, v, t, threads, p.d, g);
 #pragma unroll
         for (int j = 0; j < 4; ++j) { w[j] = mul2(w[j], g[j]); b[j] = mul2(b[j], g[j]); }
     }

@@ -15,7 +15,7 @@ struct ResNorm {
 
 cudaError_t launch_residual_norm_forward(const ResNorm& a, cudaStream_t stream);
 cudaError_t launch_residual_norm_backward(const ResNorm& a, float* partial, int accumulate, cudaStream_t stream);
-// Blocks of the backward pass: each leaves four vectors of d partial column sums.
+// Most blocks of the backward pass: each leaves four vectors of d partial column sums.
 int residual_norm_parts(int T, int d);
 
 }  // namespace bigmac
