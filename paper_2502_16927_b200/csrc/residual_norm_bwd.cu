@@ -17,7 +17,7 @@ enum { IN_X = 0, IN_Y, IN_DR, IN_DN, IN_GATE, IN_COUNT };
 // channel gate is part of them.  Without (rows of more than 4096 columns): everything loaded when it is needed.
 // GATE (of bigmac_gate_t, kNoBlock, kAnyGate) and DN are fixed at compile time for RING: with the choice at run time a row took twice the
 // instructions.  BIAS: the sums that only biases need are kept, too; without them there is room for 16 columns a thread, and half the threads of a
-// row are a third fewer instructions for it (16384 rows of 4096, RMS norms, a full gate: 219 us with 8 columns, 179 with 16).  There, what is needed again
+// row are a third fewer instructions for it (16384 rows of 4096, RMS norms, a full gate: 219 us with 8 columns, 183 with 16).  There, what is needed again
 // behind a sum is read again from shared memory; with 8 columns it is held in registers (16384 rows of 2048, LayerNorms: 101 us, read again 118).
 template <typename T, int NV, bool VEC, bool RING, int GATE, bool DN, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Params p, int threads, int stages) {
@@ -211,25 +211,25 @@ __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Pa
         if constexpr (RING) wait_groups(0);
     }
     if (!p.partial) return;
-    // the block's sums: those of its rows of threads, in order (shared memory as [groups][d] floats, one quantity after the other)
+    // the block's sums: those of its rows of threads, in order (shared memory as [groups][d] floats, one quantity after the other).  Places worked
+    // out again: the loop above has no register for them
+    int tid;
+    asm volatile("mov.u32 %0, %%tid.x;" : "=r"(tid));
+    const int own = tid % threads, own_group = tid / threads, all = kThreads / threads;
     float* tile = (float*)smem;
 #pragma unroll
-    for (int which = 0; which < 4; ++which) {
+    for (int which = 0; which < 4; which += BIAS ? 1 : 2) {
         float* out = p.partial + ((size_t)blockIdx.x * 4 + which) * p.d;
-        if (!BIAS && (which & 1)) {                                    // nobody wants them
-            for (int c = threadIdx.x; c < p.d; c += kThreads) out[c] = 0.0f;
-            continue;
-        }
         const f2* mine = which == 0 ? sum_post_w : which == 1 ? sum_post_b : which == 2 ? sum_pre_w : sum_pre_b;
         __syncthreads();
-        if (working) {
+        if (own_group < all) {
 #pragma unroll
-            for (int v = 0; v < NV; ++v) store8<float, VEC>(tile + (size_t)group * p.d, v, t, threads, p.d, mine + 4 * v);
+            for (int v = 0; v < NV; ++v) store8<float, VEC>(tile + (size_t)own_group * p.d, v, own, threads, p.d, mine + 4 * v);
         }
         __syncthreads();
-        for (int c = threadIdx.x; c < p.d; c += kThreads) {
+        for (int c = tid; c < p.d; c += kThreads) {
             float sum = 0.0f;
-            for (int i = 0; i < groups; ++i) sum += tile[(size_t)i * p.d + c];
+            for (int i = 0; i < all; ++i) sum += tile[(size_t)i * p.d + c];
             out[c] = sum;
         }
     }
@@ -238,7 +238,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Pa
 struct ParamGrads {
     float *dw_post, *db_post, *dw_pre, *db_pre, *dgate;               // dgate: of a channel gate
     const float *w_post, *b_post, *gate;                              // gate: a channel gate
-    int accumulate;
+    int accumulate, bias;                                             // bias: the parts hold the sums that only biases need
 };
 
 // Column sums of the blocks' parts, 32 columns a block; the parts are added in a fixed order.
@@ -260,11 +260,11 @@ __global__ void __launch_bounds__(1024) residual_norm_sums_kernel(const float* _
     };
     auto put = [&](float* to, float v) { if (to && threadIdx.y == 0 && c < d) to[c] = g.accumulate ? to[c] + v : v; };
     if (which == 1) {
-        const float w = total(2), b = total(3);
+        const float w = total(2), b = g.bias ? total(3) : 0.0f;
         put(g.dw_pre, w);
         put(g.db_pre, b);
     } else {
-        const float w = total(0), b = total(1);
+        const float w = total(0), b = g.bias ? total(1) : 0.0f;
         const float gate = g.gate && c < d ? g.gate[c] : 1.0f;
         put(g.dw_post, gate * w);
         put(g.db_post, gate * b);
@@ -351,7 +351,7 @@ cudaError_t launch_residual_norm_backward(const ResNorm& a, float* partial, int 
     if (!any) return cudaSuccess;
     // without rows, or without their source, the sums are zero: no parts
     const float* gate = q.gate_kind == BIGMAC_GATE_CHANNEL ? (const float*)q.gate.p : nullptr;
-    const ParamGrads g{q.dw_post, q.db_post, q.dw_pre, q.db_pre, channel, q.w_post, q.b_post, gate, accumulate};
+    const ParamGrads g{q.dw_post, q.db_post, q.dw_pre, q.db_pre, channel, q.w_post, q.b_post, gate, accumulate, wants_bias(q)};
     return launch_chained(residual_norm_sums_kernel, dim3((q.d + 31) / 32, 2), dim3(32, 32), 0, stream, partial, post || pre ? parts : 0, q.d, g);
 }
 
