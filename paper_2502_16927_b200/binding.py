@@ -371,6 +371,11 @@ def _here() -> int:
     return _current_device() if _current_device is not None else torch.cuda.current_device()
 
 
+@functools.lru_cache(maxsize=None)
+def _device(index: int) -> torch.device:
+    return torch.device("cuda", index)
+
+
 def _dense(t: torch.Tensor, name: str, here: int) -> int:
     if t.get_device() != here or here < 0 or not t.is_contiguous():
         raise ValueError(f"{name}: a dense tensor on the current device, cuda:{here}, is needed")
@@ -535,7 +540,7 @@ class Mx4:
     """A matrix in microscaled 4-bit floating point (bigmac_mx4_t): codes [rows, K / 2] and scales [row tiles, K tiles, 512] of one
     matrix, both with a leading E for the stacked weights of E experts; with `offsets` (int32 [E + 1]) the segments of a routing's
     experts, `rows` rows in the caller's order."""
-    __slots__ = ("codes", "scales", "offsets", "rows", "_c", "_device")
+    __slots__ = ("_codes", "_scales", "_room", "offsets", "rows", "_c", "_device")
 
     def __init__(self, codes: torch.Tensor, scales: torch.Tensor, offsets: Optional[torch.Tensor] = None, rows: Optional[int] = None):
         shape = codes.shape
@@ -554,12 +559,38 @@ class Mx4:
             E, table = _offsets(offsets, device), offsets.data_ptr()
             if stored < _mx4_stored(rows, E):
                 raise ValueError(f"Mx4: {rows} rows of {E} experts need {_mx4_stored(rows, E)} rows of codes")
-        self._keep(codes, scales, offsets, rows, device,
-                   bigmac_mx4_t(_dense(codes, "codes", device), _dense(scales, "scales", device), rows, 2 * half, E, table))
+        self._codes, self._scales, self._room, self.offsets, self.rows, self._device = codes, scales, None, offsets, rows, device
+        self._c = bigmac_mx4_t(_dense(codes, "codes", device), _dense(scales, "scales", device), rows, 2 * half, E, table)
 
-    def _keep(self, codes, scales, offsets, rows, device, c):
-        self.codes, self.scales, self.offsets, self.rows, self._device, self._c = codes, scales, offsets, rows, device, c
-        return self
+    @classmethod
+    def _empty(cls, stored: int, rows: int, K: int, offsets, E: int, table, device, here: int) -> "Mx4":
+        """Room for a result: one allocation, codes and scales as tensors only when they are asked for."""
+        q = cls.__new__(cls)
+        code_bytes = stored * (K // 2)
+        q._room = torch.empty_strided((code_bytes + -(-stored // 128) * -(-K // 128) * 512,), (1,), dtype=torch.uint8, device=device)
+        at = q._room.data_ptr()
+        q._codes = q._scales = None
+        q.offsets, q.rows, q._device = offsets, rows, here
+        q._c = bigmac_mx4_t(at, at + code_bytes, rows, K, E, table)
+        return q
+
+    def _views(self):
+        half = self._c.K // 2
+        stored = _mx4_stored(self.rows, self._c.E) if self.offsets is not None else self.rows
+        self._codes = self._room[:stored * half].view(stored, half)
+        self._scales = self._room[stored * half:].view(-(-stored // 128), -(-half // 64), 512)
+
+    @property
+    def codes(self) -> torch.Tensor:
+        if self._codes is None:
+            self._views()
+        return self._codes
+
+    @property
+    def scales(self) -> torch.Tensor:
+        if self._scales is None:
+            self._views()
+        return self._scales
 
 
 def _mx4(q: Mx4, here: int) -> bigmac_mx4_t:
@@ -598,16 +629,15 @@ def mx4_quantize(x: torch.Tensor, offsets: Optional[torch.Tensor] = None, slot_o
     if offsets is not None:
         E, table = _offsets(offsets, here), offsets.data_ptr()
         stored = _mx4_stored(rows, E)
-    codes, scales = _empty_mx4(stored, K, x.device)
-    q = bigmac_mx4_t(codes.data_ptr(), scales.data_ptr(), rows, K, E, table)
-    _check(lib().bigmac_mx4_quantize(ptr, _dtype(x.dtype), x_rows, ld, slots, k, C.byref(q), _stream()), "bigmac_mx4_quantize")
-    return Mx4.__new__(Mx4)._keep(codes, scales, offsets, rows, here, q)
+    q = Mx4._empty(stored, rows, K, offsets, E, table, x.device, here)
+    _check(lib().bigmac_mx4_quantize(ptr, _dtype(x.dtype), x_rows, ld, slots, k, C.byref(q._c), _stream()), "bigmac_mx4_quantize")
+    return q
 
 
-def _output(out, rows: int, columns: int, dtype, device, here: int):
+def _output(out, rows: int, columns: int, dtype, here: int):
     """The result's matrix: (tensor, address, row stride, bigmac_dtype_t)."""
     if out is None:
-        out = _new(rows, columns, dtype, device)
+        out = _new(rows, columns, dtype, _device(here))
         return out, out.data_ptr(), columns, _dtype(dtype)
     if out.shape != (rows, columns):
         raise ValueError(f"out has shape {tuple(out.shape)}, not {(rows, columns)}")
@@ -618,7 +648,7 @@ def mx4_dequantize(q: Mx4, dtype: torch.dtype = torch.bfloat16, out: Optional[to
     """The numbers a matrix stands for, in the caller's order of rows.  Of a grouped one, rows in no segment keep what `out` holds."""
     here = _here()
     c = _mx4(q, here)
-    out, ptr, ld, kind = _output(out, c.rows, c.K, dtype, q.codes.device, here)
+    out, ptr, ld, kind = _output(out, c.rows, c.K, dtype, here)
     _check(lib().bigmac_mx4_dequantize(C.byref(c), ptr, kind, ld, _stream()), "bigmac_mx4_dequantize")
     return out
 
@@ -627,15 +657,9 @@ def mx4_matmul(a: Mx4, w: Mx4, act: int = 3, dtype: torch.dtype = torch.bfloat16
     """act(a w^T) (bigmac_mx4_matmul; act a bigmac_act_t, 3 the identity).  For a grouped `a`, `w` holds the matrices of its experts."""
     here = _here()
     ca, cw = _mx4(a, here), _mx4(w, here)
-    out, ptr, ld, kind = _output(out, ca.rows, cw.rows, dtype, a.codes.device, here)
+    out, ptr, ld, kind = _output(out, ca.rows, cw.rows, dtype, here)
     _check(lib().bigmac_mx4_matmul(C.byref(ca), C.byref(cw), act, kind, ptr, ld, _stream()), "bigmac_mx4_matmul")
     return out
-
-
-def _empty_mx4(stored: int, K: int, device):
-    k_tiles = -(-K // 128)
-    return (_new(stored, K // 2, torch.uint8, device),
-            torch.empty_strided((-(-stored // 128), k_tiles, 512), (k_tiles * 512, 512, 1), dtype=torch.uint8, device=device))
 
 
 def mx4_matmul_mx4(a: Mx4, w: Mx4, act: int = 3) -> Mx4:
@@ -644,10 +668,10 @@ def mx4_matmul_mx4(a: Mx4, w: Mx4, act: int = 3) -> Mx4:
     ca, cw = _mx4(a, here), _mx4(w, here)
     if cw.rows == 0 or cw.rows % 32:
         raise ValueError(f"{cw.rows} columns: blocks of 32")
-    codes, scales = _empty_mx4(a.codes.shape[0], cw.rows, a.codes.device)
-    out = bigmac_mx4_t(codes.data_ptr(), scales.data_ptr(), ca.rows, cw.rows, ca.E, ca.offsets)
-    _check(lib().bigmac_mx4_matmul_mx4(C.byref(ca), C.byref(cw), act, C.byref(out), _stream()), "bigmac_mx4_matmul_mx4")
-    return Mx4.__new__(Mx4)._keep(codes, scales, a.offsets, a.rows, here, out)
+    stored = ca.rows if a.offsets is None else _mx4_stored(ca.rows, ca.E)
+    out = Mx4._empty(stored, ca.rows, cw.rows, a.offsets, ca.E, ca.offsets, _device(here), here)
+    _check(lib().bigmac_mx4_matmul_mx4(C.byref(ca), C.byref(cw), act, C.byref(out._c), _stream()), "bigmac_mx4_matmul_mx4")
+    return out
 
 
 def mx4_quantize_weights(w: torch.Tensor) -> Mx4:

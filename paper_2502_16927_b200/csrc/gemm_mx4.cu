@@ -201,7 +201,8 @@ cudaError_t launch(const Mx4View& a, const Mx4View& w, Mx4Params p, int64_t max_
     if (!make_map_u8(&ma, a.codes, row, a_rows, row, 128, p.box_rows, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_map_u8(&mw, w.codes, row, w_rows, row, 128, BN, CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
-    p.tma_store = OUT <= OUT_BF16_ACT && p.ldc % 8 == 0 && (uintptr_t)p.C % 16 == 0;
+    // (few rows are written as they are: a tensor map takes half a microsecond of the host's time)
+    p.tma_store = OUT <= OUT_BF16_ACT && p.M > 32 && p.ldc % 8 == 0 && (uintptr_t)p.C % 16 == 0;
     mc = mw;
     if (p.tma_store && !make_map(&mc, p.C, (uint64_t)p.N, (uint64_t)p.M, (uint64_t)p.ldc, S::kCols, 32,
                                  S::kCols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))
