@@ -202,7 +202,7 @@ cudaError_t launch(const Mx4View& a, const Mx4View& w, Mx4Params p, int64_t max_
         !make_map_u8(&mw, w.codes, row, w_rows, row, 128, BN, CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
     // (few rows are written as they are: a tensor map takes half a microsecond of the host's time)
-    p.tma_store = OUT <= OUT_BF16_ACT && p.M > 32 && p.ldc % 8 == 0 && (uintptr_t)p.C % 16 == 0;
+    p.tma_store = OUT <= OUT_BF16_ACT && p.M > 32 && tma_store_ok(p);
     mc = mw;
     if (p.tma_store && !make_map(&mc, p.C, (uint64_t)p.N, (uint64_t)p.M, (uint64_t)p.ldc, S::kCols, 32,
                                  S::kCols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B))

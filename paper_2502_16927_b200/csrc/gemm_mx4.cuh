@@ -27,6 +27,10 @@ struct Mx4Params {
     int* status;
 };
 
+// May rows of bf16 leave by TMA?  Rows on 16-byte boundaries, and whole 16 bytes of columns: a store that the tensor map cuts off inside a
+// 16-byte piece writes the rest of the piece, too, which belongs to whoever has the columns behind C.
+inline bool tma_store_ok(const Mx4Params& p) { return p.ldc % 8 == 0 && p.N % 8 == 0 && (uintptr_t)p.C % 16 == 0; }
+
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)) : "memory");

@@ -192,7 +192,7 @@ cudaError_t launch_pair(const Mx4View& a, const Mx4View& w, Mx4Params p, cudaStr
     if (!make_map_u8(&ma, a.codes, row, p.M, row, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B) || !make_map_u8(&mw, w.codes, row, p.N, row, 128, 128, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !make_map_scales(&msa, a.scales, (uint64_t)(p.M + 127) / 128 * ktiles) || !make_map_scales(&msw, w.scales, (uint64_t)(p.N + 127) / 128 * ktiles))
         return cudaErrorInvalidValue;
-    p.tma_store = OUT <= OUT_BF16_ACT && p.ldc % 8 == 0 && (uintptr_t)p.C % 16 == 0;
+    p.tma_store = OUT <= OUT_BF16_ACT && tma_store_ok(p);
     mc = mw;
     if (p.tma_store && !make_map(&mc, p.C, (uint64_t)p.N, (uint64_t)p.M, (uint64_t)p.ldc, 64, 32, CU_TENSOR_MAP_SWIZZLE_128B)) return cudaErrorInvalidValue;
     static PerDeviceOnce once;

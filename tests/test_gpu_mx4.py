@@ -350,3 +350,24 @@ def test_binding_refuses_what_is_no_4_bit_matrix(binding):
         binding.mx4_matmul_mx4(q, w)                                     # eight columns are no block
     with pytest.raises(binding.BigmacError):
         binding.mx4_matmul(q, binding.mx4_quantize(torch.zeros(8, 32, device="cuda")))
+
+
+@pytest.mark.parametrize("M,N,E,tile", [(97, 3, 0, 0), (300, 100, 0, 64), (300, 130, 0, 128), (700, 300, 0, 256), (200, 100, 4, 0), (2600, 65, 8, 0)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_columns_behind_the_result_stay(binding, M, N, E, tile, dtype):
+    """A result that is a part of a wider matrix, its rows on 16-byte boundaries and its columns not: the others' columns are left alone."""
+    rng = _gen(29)
+    K = 96
+    _, _, codes, scales = _weights(rng, (E,) if E else (), N, K)
+    offsets = torch.from_numpy(_segments(rng, E, M, "skewed").astype(np.int32)).cuda() if E else None
+    q = binding.mx4_quantize(torch.from_numpy(rng.standard_normal((M, K))).to("cuda", torch.bfloat16), offsets=offsets)
+    W = binding.Mx4(codes, scales)
+    wide = torch.full((M + 2, (N + 23) // 8 * 8), 5.0, dtype=dtype, device="cuda")
+    binding.bigmac_debug_set("mx4_tile", tile)
+    try:
+        binding.mx4_matmul(q, W, out=wide[:M, :N])
+        alone = binding.mx4_matmul(q, W, dtype=dtype)
+    finally:
+        binding.bigmac_debug_set("defaults", 0)
+    assert torch.equal(wide[:M, :N], alone)
+    assert bool((wide[:, N:] == 5.0).all()) and bool((wide[M:] == 5.0).all())
