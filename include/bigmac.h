@@ -316,7 +316,7 @@ int bigmac_operator_status(void *stream);
  * Matrices are [T, d] of dtype with rows `ld` elements apart; parameters, their gradients, row gates and stats are fp32.  Pointers
  * are aligned to their element type; d a multiple of 8 with every pointer and row on a 16-byte boundary runs on 16-byte accesses, anything
  * else on single elements.  d <= 8192, T <= 2^30, ld < 2^31.  r may be x and n may be y (same pointer and ld), dx may be dr and dy may
- * be dn; other overlaps of inputs and outputs are errors of the caller. */
+ * be dn; other overlaps of inputs and outputs are errors of the caller; two gradients of vectors in one place are refused. */
 typedef enum { BIGMAC_NORM_NONE = 0, BIGMAC_NORM_RMS = 1, BIGMAC_NORM_LAYER = 2 } bigmac_norm_t;
 typedef enum { BIGMAC_GATE_NONE = 0, BIGMAC_GATE_TOKEN = 1, BIGMAC_GATE_CHANNEL = 2, BIGMAC_GATE_FULL = 3 } bigmac_gate_t;
 typedef struct {

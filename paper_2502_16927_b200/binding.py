@@ -376,6 +376,9 @@ def _device(index: int) -> torch.device:
     return torch.device("cuda", index)
 
 
+_MOST_ROWS = 0x7fffffff                                 # int32_t of the C calls
+
+
 def _dense(t: torch.Tensor, name: str, here: int) -> int:
     if t.get_device() != here or here < 0 or not t.is_contiguous():
         raise ValueError(f"{name}: a dense tensor on the current device, cuda:{here}, is needed")
@@ -384,14 +387,14 @@ def _dense(t: torch.Tensor, name: str, here: int) -> int:
 
 def _matrix(t: torch.Tensor, shape, name: str, here: int):
     """(address, row stride) of a matrix with dense rows; shape is t.shape."""
-    if t.get_device() == here and len(shape) == 2:
+    if t.get_device() == here and len(shape) == 2 and shape[0] <= _MOST_ROWS:
         if t.is_contiguous():
             return t.data_ptr(), shape[1]
         rows, columns = shape
         ld, step = t.stride()
         if (step == 1 or columns == 1) and (ld >= columns or rows == 1):
             return t.data_ptr(), max(ld, columns)
-    raise ValueError(f"{name}: a matrix with dense rows that do not overlap, on the current device, cuda:{here}, is needed")
+    raise ValueError(f"{name}: a matrix with dense rows (2^31 - 1 at most) that do not overlap, on the current device, cuda:{here}, is needed")
 
 
 def _new(rows: int, columns: int, dtype, device) -> torch.Tensor:
@@ -559,6 +562,8 @@ class Mx4:
             E, table = _offsets(offsets, device), offsets.data_ptr()
             if stored < _mx4_stored(rows, E):
                 raise ValueError(f"Mx4: {rows} rows of {E} experts need {_mx4_stored(rows, E)} rows of codes")
+        if not 0 <= rows <= _MOST_ROWS:
+            raise ValueError(f"Mx4: {rows} rows")
         self._codes, self._scales, self._room, self.offsets, self.rows, self._device = codes, scales, None, offsets, rows, device
         self._c = bigmac_mx4_t(_dense(codes, "codes", device), _dense(scales, "scales", device), rows, 2 * half, E, table)
 
@@ -622,7 +627,7 @@ def mx4_quantize(x: torch.Tensor, offsets: Optional[torch.Tensor] = None, slot_o
     if K == 0 or K % 32:
         raise ValueError(f"K = {K}: blocks of 32 columns")
     if slot_of_row is not None:
-        if slot_of_row.dtype is not torch.int32 or slot_of_row.dim() != 1:
+        if slot_of_row.dtype is not torch.int32 or slot_of_row.dim() != 1 or slot_of_row.shape[0] > _MOST_ROWS:
             raise ValueError("slot_of_row: an int32 vector is needed")
         slots, rows = _dense(slot_of_row, "slot_of_row", here), slot_of_row.shape[0]
     stored = rows
@@ -710,6 +715,7 @@ class Layer:
         self._saved = None
         self._need = {}
         self._T = None
+        self._steps = 0                                 # training forwards so far
 
     def close(self):
         if self.handle is not None:
@@ -787,6 +793,7 @@ class Layer:
         R = self.empty_routing(T) if want_routing else None
         bigmac_forward(self.handle, x, T, W, y, R, self._saved if training else None, self._scratch)
         self._T = T if training else None
+        self._steps += training
         return (y, R) if want_routing else y
 
     def backward(self, x, dy, W, G, dx=None, accumulate=False):
@@ -804,7 +811,8 @@ class Layer:
 
 class Block:
     """The layer as a residual block: out = residual_scale x + gate N_post(layer(N_pre(x))), forward and backward, with the two joints of
-    residual_norm_forward around it.  pre, post: `Norm`s (post may be None); gate: a vector of parameters [d], or None."""
+    residual_norm_forward around it.  pre, post: `Norm`s (post may be None); gate: a vector of parameters [d], or None.  A backward follows
+    the training forward whose gradients it gives: the layer keeps one step."""
 
     def __init__(self, layer: Layer, pre: Norm, post: Optional[Norm] = None, gate: Optional[torch.Tensor] = None, residual_scale: float = 1.0):
         self.layer, self.pre, self.post, self.gate, self.residual_scale = layer, pre, post, gate, residual_scale
@@ -816,7 +824,7 @@ class Block:
         y = self.layer.forward(n, W, training=training, want_routing=want_routing)
         y, R = y if want_routing else (y, None)
         out, _, after = residual_norm_forward(x, y, self.gate, self.post, residual_scale=self.residual_scale, training=training, gate_kind=self._gate_kind)
-        self._kept = (x, n, y, before, after) if training else None
+        self._kept = (x, n, y, before, after, self.layer._steps) if training else None
         return (out, R) if want_routing else out
 
     def backward(self, dout, W, G, accumulate=False):
@@ -824,7 +832,9 @@ class Block:
         dgate."""
         if self._kept is None:
             raise RuntimeError("backward needs a training forward first")
-        x, n, y, before, after = self._kept
+        x, n, y, before, after, step = self._kept
+        if step != self.layer._steps:
+            raise RuntimeError("the layer keeps one step: another training forward of it came between")
         own = {name: G[name] for name in ("dw_post", "db_post", "dgate") if name in G}
         dx, dy, _ = residual_norm_backward(x, y, self.gate, self.post, None, dout, None, after, own, self.residual_scale, accumulate, self._gate_kind)
         dn = self.layer.backward(n, dy, W, G, accumulate=accumulate)

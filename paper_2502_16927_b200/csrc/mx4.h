@@ -38,6 +38,7 @@ struct Mx4Segments {
             const int lane = threadIdx.x, per = (E + 31) / 32, e0 = min(E, lane * per), e1 = min(E, e0 + per);
             int mine = 0;
             for (int e = e0; e < e1; ++e) mine += tiles_of(e);
+            mine = min(mine, 1 << 25);                 // twice what memory has room for: the sum over a table that is none stays in 32 bits
             int run = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {

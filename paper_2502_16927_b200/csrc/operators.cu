@@ -1,5 +1,6 @@
 // C-ABI entry points of the operators around the layer: argument checks and launches.
 #include <cmath>
+#include <initializer_list>
 
 #include "bigmac.h"
 #include "internal.h"
@@ -44,6 +45,13 @@ Mx4View view_of(const bigmac_mx4_t* q) {
     return Mx4View{(uint8_t*)q->codes, (uint8_t*)q->scales, q->rows, q->K, q->E, q->offsets, capacity};
 }
 
+// No two sums in one place (the gradients of a vector that both norms share need two).
+bool apart(std::initializer_list<const void*> sums) {
+    for (auto a = sums.begin(); a != sums.end(); ++a)
+        for (auto b = a + 1; b != sums.end(); ++b)
+            if (*a && *a == *b) return false;
+    return true;
+}
 // A matrix of the joint: aligned to its elements, rows that do not overlap.  *vec: rows on 16-byte boundaries, too.
 bool rows_ok(const bigmac_rows_t& m, int64_t d, int64_t es, bool* vec) {
     if (!m.p) return true;
@@ -87,6 +95,7 @@ int check_residual_norm(const bigmac_residual_norm_t* q, int32_t T, bool backwar
     if (!ok || (!q->y.p && q->dy.p) || (q->pre_kind == BIGMAC_NORM_NONE && q->dn.p))
         return BIGMAC_ERR_INVALID_ARG;
     if (!q->stats || (!q->dr.p && !q->dn.p)) return BIGMAC_ERR_INVALID_ARG;
+    if (!apart({q->dw_post, q->db_post, q->dw_pre, q->db_pre, q->dgate.p})) return BIGMAC_ERR_INVALID_ARG;
     return BIGMAC_OK;
 }
 size_t residual_norm_scratch(const bigmac_residual_norm_t* q, int32_t T) {
@@ -180,9 +189,10 @@ int bigmac_mx4_matmul_mx4(const bigmac_mx4_t* a, const bigmac_mx4_t* w, int32_t 
     if (s == BIGMAC_OK) s = check_mx4(out, false);
     if (s != BIGMAC_OK) return s;
     if (act < 0 || act > BIGMAC_ACT_IDENTITY || w->offsets || a->K != w->K || a->E != w->E || out->rows != a->rows || out->K != w->rows ||
-        out->E != a->E || out->offsets != a->offsets || out->codes == a->codes || out->scales == a->scales)
+        out->E != a->E || out->offsets != a->offsets)
         return BIGMAC_ERR_INVALID_ARG;
     if (a->rows == 0) return BIGMAC_OK;
+    if (out->codes == a->codes || out->scales == a->scales) return BIGMAC_ERR_INVALID_ARG;
     int* status = status_word();
     if (!status) return BIGMAC_ERR_CUDA;
     const Mx4View to = view_of(out);

@@ -103,3 +103,16 @@ def test_block_with_4_bit_experts():
     want = binding.residual_norm_forward(dev["x"], y, block.gate, block.post, None, residual_scale=0.8, gate_kind=binding.BIGMAC_GATE_CHANNEL)[0]
     assert torch.equal(out, want) and torch.equal(R["topk_idx"], layer.route(n, dev)["topk_idx"])
     layer.close()
+
+
+def test_two_steps_of_one_layer_at_once_are_refused():
+    """The layer keeps one step: gradients of the one before would be those of the wrong activations."""
+    binding, w, dev, layer, block = _block(wl.DTYPE_F32, seed=75)
+    G = _grads(w, dev)
+    other = binding.Block(layer, block.pre)
+    block.forward(dev["x"], dev, training=True)
+    other.forward(dev["x"], dev, training=True)
+    with pytest.raises(RuntimeError):
+        block.backward(dev["dy"], dev, G)
+    other.backward(dev["dy"], dev, G)
+    layer.close()

@@ -108,3 +108,39 @@ def test_tables_that_are_no_segments_touch_nothing_else(binding):
         torch.cuda.synchronize()
         assert bool((out[rows:] == 7.0).all()) and bool((back[rows:] == 7.0).all())
     assert binding.operator_status() == 0
+
+
+def test_tables_whose_counts_pass_32_bits(binding):
+    """A table of 512 full segments of all rows, more tiles than 32 bits count: nothing but the results is written."""
+    E, rows, K, N = 1024, (1 << 29) + 100, 32, 8
+    offsets = torch.tensor([0, rows] * (E // 2) + [0], dtype=torch.int32, device="cuda")
+    x = torch.ones(1, K, dtype=torch.bfloat16, device="cuda")
+    q = binding.mx4_quantize(x, offsets=offsets, slot_of_row=torch.zeros(rows, dtype=torch.int32, device="cuda"))
+    w = binding.mx4_quantize_weights(torch.randn(1, N, K, device="cuda"))
+    w = binding.Mx4(w.codes.expand(E, -1, -1).contiguous(), w.scales.expand(E, -1, -1, -1).contiguous())
+    guard = 1 << 20
+    room = torch.zeros(rows + 2 * guard, N, dtype=torch.bfloat16, device="cuda")
+    binding.mx4_matmul(q, w, out=room[guard:guard + rows])
+    torch.cuda.synchronize()
+    assert not bool(room[:guard].any()) and not bool(room[guard + rows:].any())
+    assert binding.operator_status() == 0
+
+
+def test_rows_that_pass_32_bits_are_refused(binding):
+    x = torch.empty((1 << 32) + 5, 1, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ValueError):
+        binding.residual_norm_forward(x, pre=binding.Norm(binding.BIGMAC_NORM_RMS))
+    with pytest.raises(binding.BigmacError):
+        binding.residual_norm_forward(x[:(1 << 30) + 1], pre=binding.Norm(binding.BIGMAC_NORM_RMS))
+    with pytest.raises(ValueError):
+        binding.Mx4(torch.empty((1 << 31) + 128, 1, dtype=torch.uint8, device="cuda"), torch.empty((1 << 24) + 1, 1, 512, dtype=torch.uint8, device="cuda"))
+
+
+def test_4_bit_products_of_no_rows(binding):
+    q, w = binding.mx4_quantize(torch.empty(0, 64, device="cuda")), binding.mx4_quantize(torch.randn(96, 64, device="cuda"))
+    h = binding.mx4_matmul_mx4(q, w)
+    assert h.rows == 0 and binding.mx4_dequantize(h).shape == (0, 96)
+    offsets = torch.zeros(5, dtype=torch.int32, device="cuda")
+    grouped = binding.mx4_quantize(torch.empty(0, 64, device="cuda"), offsets=offsets)
+    h = binding.mx4_matmul_mx4(grouped, binding.mx4_quantize_weights(torch.randn(4, 96, 64, device="cuda")))
+    assert h.rows == 0 and binding.mx4_dequantize(h).shape == (0, 96)

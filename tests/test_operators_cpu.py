@@ -91,6 +91,12 @@ def test_mx4_dequantize_and_matmul_refusals(lib):
     assert product(a=_mx4(rows=0)) == 0 and product(w=_mx4(rows=0)) == 0
 
 
+def test_mx4_products_of_no_rows(lib):
+    empty, w = binding.bigmac_mx4_t(None, None, 0, 64, 0, None), _mx4(rows=32)
+    assert lib.bigmac_mx4_matmul_mx4(C.byref(empty), C.byref(w), 3, C.byref(binding.bigmac_mx4_t(None, None, 0, 32, 0, None)), None) == 0
+    assert lib.bigmac_mx4_matmul(C.byref(empty), C.byref(w), 3, 0, None, 32, None) == 0
+
+
 def test_binding_refuses_what_is_no_4_bit_matrix():
     u8 = torch.uint8
     for codes, scales, kw in ((torch.zeros(4, 32), torch.zeros(1, 1, 512, dtype=u8), {}),
@@ -157,6 +163,12 @@ def test_residual_norm_refusals(lib):
                       dict(y=0, post_kind=0), dict(dw_post=HERE + 1), dict(dw_post=HERE, scratch=None), dict(dw_post=HERE, scratch=HERE + 8)]:
         assert call(**kw) == -1, kw
     assert call(dw_post=HERE, size=16) == -3
+
+    sums = dict(dw_post=2 * HERE, db_post=3 * HERE, dw_pre=4 * HERE, db_pre=5 * HERE)                     # a vector that both norms share: two sums
+    for pair in (("dw_post", "dw_pre"), ("db_post", "db_pre"), ("dw_pre", "db_pre")):
+        assert call(**{**sums, pair[1]: sums[pair[0]]}) == -1, pair
+    assert call(**sums, gate_kind=2, gate=HERE, dgate=2 * HERE) == -1
+    assert call(**sums, size=16) == -3
 
     need = C.c_size_t()
     assert lib.bigmac_residual_norm_scratch_bytes(_joint(**back), 4, C.byref(need)) == 0 and need.value == 0
