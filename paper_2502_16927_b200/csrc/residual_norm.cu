@@ -21,13 +21,13 @@ namespace {
 
 // Few rows, or rows of more than 4096 columns: one row to `threads` threads, 8 NV columns each.  Rows of a warp may share a block,
 // longer ones have one for themselves.
-template <typename T, int NV, bool VEC>
+template <typename T, int NV, int VEC>
 __global__ void __launch_bounds__(1024 / NV) residual_norm_kernel(const Params p, int threads) {
-    __shared__ float sums[2][32];
+    __shared__ __align__(16) float sums[2][32];
     grid_dependency_launch();
     grid_dependency_wait();
     const int in_block = threads == 32 ? threadIdx.x >> 5 : 0;
-    Row at{sums[0], sums[1], threads == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads, 1};
+    Row at(sums[0], sums[1], threads == 32 ? (int)threadIdx.x & 31 : (int)threadIdx.x, threads, 1);
     const int t = at.t;
     const int row = (int)blockIdx.x * (threads == 32 ? (int)blockDim.x >> 5 : 1) + in_block;
     if (row >= p.T) return;
@@ -91,24 +91,24 @@ __global__ void __launch_bounds__(1024 / NV) residual_norm_kernel(const Params p
 // Many rows: persistent blocks of 512 threads, two on an SM, `threads` of them to a row, eight columns a thread.  A block a row spent 2 us
 // of an SM on a row of 4096 columns whatever its type, all of it latencies one after the other (loads, sums, parameters, sums); here the next rows are on
 // their way meanwhile and the parameters stay in shared memory.
-template <typename T, bool VEC, int GATE>
+template <typename T, int VEC, int GATE>
 __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const Params p, int threads, int stages, int vectors) {
     extern __shared__ __align__(16) uint8_t smem[];
     constexpr int COUNT = GATE == kNoBlock ? 1 : GATE == BIGMAC_GATE_FULL ? 3 : 2;
-    __shared__ float sums[2][kThreads / 32][32];
+    __shared__ __align__(16) float sums[2][kThreads / 32][32];
     grid_dependency_launch();
     grid_dependency_wait();
     const int t = threadIdx.x % threads, group = threadIdx.x / threads, groups = kThreads / threads;
     if (group >= groups) return;                                       // threads that are no whole row
     const int first = (int)blockIdx.x * groups + group, step = (int)gridDim.x * groups;
-    Row at{sums[0][group], sums[1][group], t, threads, 1 + group};
+    Row at(sums[0][group], sums[1][group], t, threads, 1 + group);
     Ring<T, VEC, COUNT> ring;
     const void* const in[3] = {p.x, p.y, p.gate};
     const int ld[3] = {p.x_ld, p.y_ld, p.gate_ld};
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) { ring.in[i] = (const T*)in[i]; ring.ld[i] = ld[i]; ring.has[i] = true; }
     ring.init(smem + vectors * param_bytes(false, threads, 1), group, stages, p);
-    ring.start(first, step, t, threads);
+    ring.template start<VEC>(first, step, t, threads);
     // vectors 0, 1: w and b of the norm before, 2, 3: of the one behind; b only with `vectors` = 4.
     ParamStore<1, false> par(smem, t, threads);
     const int pre = vectors / 2;
@@ -130,7 +130,8 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
     const f2 rho = pk(p.rho);
     for (int row = first; row < p.T; row += step) {
         const float token = GATE == BIGMAC_GATE_TOKEN ? ((const float*)p.gate)[row] : 1.0f;
-        ring.next(stage, row, step, at);
+        if constexpr (VEC) ring.arrived();
+        else ring.next(stage, row, step, at);
         f2 r[4];
         float4 st = make_float4(0.0f, 1.0f, 0.0f, 1.0f);
         ring.get(stage, 0, 0, row, t, threads, r);
@@ -148,8 +149,8 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
                 const f2 a = fma2(mul2(add2(y[j], pk(-st.x)), pk(st.y)), w[j], b[j]);
                 r[j] = GATE == BIGMAC_GATE_FULL ? fma2(g[j], a, r[j]) : GATE == BIGMAC_GATE_TOKEN ? fma2(pk(token), a, r[j]) : add2(a, r[j]);
             }
-            cut8<VEC>(0, t, threads, p.d, r);
         }
+        if constexpr (VEC) ring.again(stage, row, step, at);
         if (p.r) store8<T, VEC>(row_at((T*)p.r, row, p.r_ld), 0, t, threads, p.d, r);
         if (p.n) {
             f2 w[4], b[4];
@@ -166,7 +167,7 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
     wait_groups(0);
 }
 
-template <typename T, int NV, bool VEC>
+template <typename T, int NV, int VEC>
 cudaError_t one_row_a_block(const ResNorm& a, cudaStream_t stream) {
     const int threads = threads_of(a.q->d, NV), rows = threads == 32 ? (a.T < 8 * gemm_tc_sm_count() ? 1 : 8) : 1;
     const int64_t grid = ((int64_t)a.T + rows - 1) / rows;
@@ -175,7 +176,7 @@ cudaError_t one_row_a_block(const ResNorm& a, cudaStream_t stream) {
 
 constexpr size_t kRowsSmem = 108 * 1024;                               // of a block, two to an SM (and 4 KB for sums)
 
-template <typename T, bool VEC, int GATE>
+template <typename T, int VEC, int GATE>
 cudaError_t persistent(const ResNorm& a, cudaStream_t stream) {
     auto kernel = residual_norm_rows_kernel<T, VEC, GATE>;
     const int threads = threads_of(a.q->d, 1), groups = kThreads / threads, count = GATE == kNoBlock ? 1 : GATE == BIGMAC_GATE_FULL ? 3 : 2;
@@ -192,7 +193,7 @@ cudaError_t persistent(const ResNorm& a, cudaStream_t stream) {
     const int64_t want = ((int64_t)a.T + groups - 1) / groups, most = 2 * (int64_t)gemm_tc_sm_count();
     return launch_chained(kernel, (int)(want < most ? want : most), kThreads, par + stages * stage, stream, params_of(a), threads, stages, vectors);
 }
-template <typename T, bool VEC>
+template <typename T, int VEC>
 cudaError_t persistent_by_gate(const ResNorm& a, cudaStream_t stream) {
     if (!a.q->y.p) return persistent<T, VEC, kNoBlock>(a, stream);
     switch (a.q->gate_kind) {
@@ -206,9 +207,9 @@ cudaError_t forward(const ResNorm& a, cudaStream_t stream) {
     const int d = a.q->d;
     const bool wide = d > 8 * kThreads;
     const int64_t rows_at_once = (int64_t)2 * gemm_tc_sm_count() * (wide ? 1 : kThreads / threads_of(d, 1));
-    if (!wide && a.T > rows_at_once && (sizeof(T) == 2 || !a.vec)) return a.vec ? persistent_by_gate<T, true>(a, stream) : persistent_by_gate<T, false>(a, stream);
-    if (!a.vec) return one_row_a_block<T, 2, false>(a, stream);
-    return wide || (sizeof(T) == 4 && a.T > rows_at_once) ? one_row_a_block<T, 2, true>(a, stream) : one_row_a_block<T, 1, true>(a, stream);
+    if (!wide && a.T > rows_at_once && (sizeof(T) == 2 || !a.vec)) return a.vec ? persistent_by_gate<T, kVecOf<T>>(a, stream) : persistent_by_gate<T, kAlternate>(a, stream);
+    if (!a.vec) return one_row_a_block<T, 2, kAlternate>(a, stream);
+    return wide || (sizeof(T) == 4 && a.T > rows_at_once) ? one_row_a_block<T, 2, kVecOf<T>>(a, stream) : one_row_a_block<T, 1, kVecOf<T>>(a, stream);
 }
 
 }  // namespace

@@ -33,10 +33,16 @@ __device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c) { f2 d; asm("fma.rn.f32x2 %
 __device__ __forceinline__ f2 mul2(f2 a, f2 b) { f2 d; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 __device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 d; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b)); return d; }
 
-// A row's elements on its threads: thread t has pieces v of eight.  VEC: eight neighbours, 16-byte accesses.  Else the threads' elements alternate, so
-// that accesses to single elements are still whole lines.
-template <bool VEC>
-__device__ __forceinline__ int column(int v, int j, int t, int threads) { return VEC ? (v * threads + t) * 8 + j : (v * 8 + j) * threads + t; }
+// A row's elements on its threads: thread t has pieces v of eight.  VEC kNeighbours: eight neighbours (a 16-byte access of bf16); kFours: four and
+// four, each a 16-byte access of fp32 next to the other threads' (eight neighbours are two accesses that use half of every 32-byte sector: backward of 8000 rows of
+// 4096 292 us).  kAlternate, for rows off 16-byte boundaries: the threads' elements alternate, so that accesses to single elements are still whole lines.
+constexpr int kAlternate = 0, kNeighbours = 1, kFours = 2;
+template <typename T>
+constexpr int kVecOf = sizeof(T) == 4 ? kFours : kNeighbours;
+template <int VEC>
+__device__ __forceinline__ int column(int v, int j, int t, int threads) {
+    return VEC == kNeighbours ? (v * threads + t) * 8 + j : VEC == kFours ? (2 * v + (j >> 2)) * 4 * threads + 4 * t + (j & 3) : (v * 8 + j) * threads + t;
+}
 
 __device__ __forceinline__ f2 pair_of(uint32_t w) { return pk(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 __device__ __forceinline__ void unpack8(const uint4& a, f2* f) { f[0] = pair_of(a.x); f[1] = pair_of(a.y); f[2] = pair_of(a.z); f[3] = pair_of(a.w); }
@@ -47,10 +53,17 @@ __device__ __forceinline__ void from_float(float v, float* p) { *p = v; }
 __device__ __forceinline__ void from_float(float v, __nv_bfloat16* p) { *p = __float2bfloat16(v); }
 
 // Eight elements of a row (zeros behind column d).
-template <typename T, bool VEC>
+template <typename T, int VEC>
 __device__ __forceinline__ void load8(const T* row, int v, int t, int threads, int d, f2* f) {
     const int c0 = column<VEC>(v, 0, t, threads);
-    if constexpr (VEC) {
+    if constexpr (VEC == kFours) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int c = column<VEC>(v, 4 * h, t, threads);
+            const ulonglong2 a = c < d ? *(const ulonglong2*)(row + c) : make_ulonglong2(0, 0);
+            f[2 * h] = a.x; f[2 * h + 1] = a.y;
+        }
+    } else if constexpr (VEC) {
         if (c0 < d) {
             if constexpr (sizeof(T) == 2) {
                 unpack8(*(const uint4*)(row + c0), f);
@@ -69,13 +82,17 @@ __device__ __forceinline__ void load8(const T* row, int v, int t, int threads, i
         for (int j = 0; j < 4; ++j) f[j] = pk(e[2 * j], e[2 * j + 1]);
     }
 }
-template <typename T, bool VEC>
+template <typename T, int VEC>
 __device__ __forceinline__ void store8(T* row, int v, int t, int threads, int d, const f2* f) {
     const int c0 = column<VEC>(v, 0, t, threads);
     float e[8];
 #pragma unroll
     for (int j = 0; j < 4; ++j) upk(f[j], e[2 * j], e[2 * j + 1]);
-    if constexpr (VEC) {
+    if constexpr (VEC == kFours) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+            if (const int c = column<VEC>(v, 4 * h, t, threads); c < d) *(ulonglong2*)(row + c) = make_ulonglong2(f[2 * h], f[2 * h + 1]);
+    } else if constexpr (VEC) {
         if (c0 >= d) return;
         if constexpr (sizeof(T) == 2) {
             uint32_t w[4];
@@ -96,10 +113,13 @@ __device__ __forceinline__ void store8(T* row, int v, int t, int threads, int d,
     }
 }
 // Zeros behind column d.
-template <bool VEC>
+template <int VEC>
 __device__ __forceinline__ void cut8(int v, int t, int threads, int d, f2* f) {
     const int c0 = column<VEC>(v, 0, t, threads);
-    if constexpr (VEC) {
+    if constexpr (VEC == kFours) {
+        if (c0 >= d) f[0] = f[1] = pk(0.0f);
+        if (column<VEC>(v, 4, t, threads) >= d) f[2] = f[3] = pk(0.0f);
+    } else if constexpr (VEC) {
         if (c0 >= d) fill8(0.0f, f);
     } else {
 #pragma unroll
@@ -111,7 +131,7 @@ __device__ __forceinline__ void cut8(int v, int t, int threads, int d, f2* f) {
     }
 }
 // A vector of parameters: `fill` where there is none.  (The pointers of VEC vectors are 16-byte aligned, too.)
-template <bool VEC>
+template <int VEC>
 __device__ __forceinline__ void param8(const float* p, float fill, int v, int t, int threads, int d, f2* f) {
     if (p) load8<float, VEC>(p, v, t, threads, d, f);
     else fill8(fill, f);
@@ -134,42 +154,50 @@ __device__ __forceinline__ float warp_sum_halves(float a, float b, bool upper) {
 // Waits for the `threads` threads of a row (whole warps of one block; id 1 .. 15).
 __device__ __forceinline__ void row_barrier(int id, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory"); }
 
-// What a row's threads have in common: their number, and room for sums, two regions in turn, so that one barrier a sum is enough.
+// What a row's threads have in common: their number, and room for sums, two regions in turn, so that one barrier a sum is enough.  A region holds
+// the warps' (16 at most) parts of two sums, zeros behind them.
 struct Row {
     float *slots, *other;
     int t, threads, id;
+    __device__ __forceinline__ Row(float* a, float* b, int t_, int threads_, int id_) : slots(a), other(b), t(t_), threads(threads_), id(id_) {
+        if (t < 16 && t >= threads >> 5) a[t] = a[16 + t] = b[t] = b[16 + t] = 0.0f;       // seen behind the first sum's barrier
+    }
     __device__ __forceinline__ void turn() { float* const s = slots; slots = other; other = s; }
 };
+// The warps' parts, read by every thread: half the latency of adding them up between lanes.
+__device__ __forceinline__ float slots_sum(const float* slots, int threads) {
+    const ulonglong2* q = (const ulonglong2*)slots;
+    f2 s = add2(q[0].x, q[0].y);
+    if (threads > 128) s = add2(s, add2(q[1].x, q[1].y));
+    if (threads > 256) s = add2(s, add2(add2(q[2].x, q[2].y), add2(q[3].x, q[3].y)));
+    return both(s);
+}
 // Sums over the threads of a row, in a fixed order.
 __device__ __forceinline__ float row_sum(float v, Row& r) {
     v = warp_sum(v);
     if (r.threads == 32) return v;
-    const int lane = r.t & 31;
-    if (lane == 0) r.slots[r.t >> 5] = v;
+    if ((r.t & 31) == 0) r.slots[r.t >> 5] = v;
     row_barrier(r.id, r.threads);
-    v = warp_sum(lane < (r.threads >> 5) ? r.slots[lane] : 0.0f);
+    v = slots_sum(r.slots, r.threads);
     r.turn();
     return v;
 }
-// Two at once; up to 16 warps.
+// Two at once.
 __device__ __forceinline__ void row_sum2(float& a, float& b, Row& r) {
     const int lane = r.t & 31;
-    const bool upper = lane >= 16;
-    float v = warp_sum_halves(a, b, upper);
+    float v = warp_sum_halves(a, b, lane >= 16);
     if (r.threads > 32) {
         if ((lane & 15) == 0) r.slots[(lane & 16) + (r.t >> 5)] = v;
         row_barrier(r.id, r.threads);
-        v = (lane & 15) < (r.threads >> 5) ? r.slots[lane] : 0.0f;
+        v = slots_sum(r.slots + (lane & 16), r.threads);
         r.turn();
-#pragma unroll
-        for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
     }
     a = __shfl_sync(kAll, v, 0);
     b = __shfl_sync(kAll, v, 16);
 }
 
 // Mean and 1 / sqrt(var + eps) of a row in registers (zeros behind column d); the variance from the differences to the mean.
-template <int NV, bool VEC>
+template <int NV, int VEC>
 __device__ __forceinline__ void row_stats(int kind, const f2* f, float eps, const Params& p, Row& row, float& mean, float& rstd) {
     mean = 0.0f;
     rstd = 1.0f;
@@ -185,9 +213,13 @@ __device__ __forceinline__ void row_stats(int kind, const f2* f, float eps, cons
             f2 e[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) e[j] = add2(f[4 * v + j], pk(-mean));
-            cut8<VEC>(v, row.t, row.threads, p.d, e);
+            if (!VEC) cut8<VEC>(v, row.t, row.threads, p.d, e);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s = fma2(e[j], e[j], s);
+            for (int h = 0; h < 2; ++h) {
+                if (VEC && column<VEC>(v, VEC == kFours ? 4 * h : 0, row.t, row.threads) >= p.d) continue;
+                s = fma2(e[2 * h], e[2 * h], s);
+                s = fma2(e[2 * h + 1], e[2 * h + 1], s);
+            }
         }
     } else {
 #pragma unroll
@@ -226,7 +258,7 @@ inline size_t stage_bytes(bool vec, int d, int es, int groups, int count, int nv
 // VEC: every thread copies and reads its own 16 bytes, so no thread waits for another.  Else a row begins anywhere: its threads copy the 16-byte
 // granules that hold it and read single elements after a barrier; the first and the last rows of all, whose granules may reach out of the
 // tensor, are read directly.
-template <typename T, bool VEC, int COUNT, int NV = 1>
+template <typename T, int VEC, int COUNT, int NV = 1>
 struct Ring {
     static constexpr int kHalves = (int)sizeof(T) / 2;                 // 16-byte pieces of eight elements
     const T* in[COUNT];
@@ -256,10 +288,9 @@ struct Ring {
                     const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot(stage, i));
 #pragma unroll
                     for (int v = 0; v < NV; ++v) {
-                        const int c = column<true>(v, 0, t, threads);
-                        if (c >= d) continue;
 #pragma unroll
-                        for (int h = 0; h < kHalves; ++h) copy16(to + (v * kHalves + h) * kPieceBytes, from + c + h * 4);
+                        for (int h = 0; h < kHalves; ++h)
+                            if (const int c = column<VEC>(v, 4 * h, t, threads); c < d) copy16(to + (v * kHalves + h) * kPieceBytes, from + c);
                     }
                 }
             } else {
@@ -276,10 +307,14 @@ struct Ring {
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
-    // Rows first, first + step, ... up to the (stages - 1)-th are asked for.
+    // The first rows are asked for; LATE: as many as there are stages, which `again` then fills.
+    template <bool LATE = false>
     __device__ __forceinline__ void start(int first, int step, int t, int threads) {
-        for (int s = 0; s < stages - 1; ++s) fetch(s, first + s * step, t, threads);
+        for (int s = 0; s < stages - (LATE ? 0 : 1); ++s) fetch(s, first + s * step, t, threads);
     }
+    // LATE (VEC): row `row` is in its stage; once it has been read, the row that is `stages` rows later comes there.
+    __device__ __forceinline__ void arrived() const { wait_groups(stages - 1); }
+    __device__ __forceinline__ void again(int stage, int row, int step, const Row& at) { fetch(stage, row + stages * step, at.t, at.threads); }
     // Row `row` is in its stage, the one stages - 1 rows later on its way.
     __device__ __forceinline__ void next(int stage, int row, int step, const Row& at) {
         if constexpr (VEC) {
@@ -303,16 +338,16 @@ struct Ring {
     __device__ __forceinline__ void get(int stage, int which, int v, int row, int t, int threads, f2* f) const {
         if (!has[which]) { fill8(0.0f, f); return; }
         if constexpr (VEC) {
-            if (column<true>(v, 0, t, threads) < d) {
-                const uint8_t* s = slot(stage, which) + v * kHalves * kPieceBytes;
-                if constexpr (sizeof(T) == 2) {
-                    unpack8(*(const uint4*)s, f);
-                } else {
-                    const ulonglong2 a = *(const ulonglong2*)s, b = *(const ulonglong2*)(s + kPieceBytes);
-                    f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
-                }
+            const uint8_t* s = slot(stage, which) + v * kHalves * kPieceBytes;
+            if constexpr (sizeof(T) == 2) {
+                if (column<VEC>(v, 0, t, threads) < d) unpack8(*(const uint4*)s, f);
+                else fill8(0.0f, f);
             } else {
-                fill8(0.0f, f);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const ulonglong2 a = column<VEC>(v, 4 * h, t, threads) < d ? *(const ulonglong2*)(s + h * kPieceBytes) : make_ulonglong2(0, 0);
+                    f[2 * h] = a.x; f[2 * h + 1] = a.y;
+                }
             }
         } else {
             const T* from = row_at(in[which], row, ld[which]);
@@ -341,8 +376,9 @@ struct ParamStore {
 };
 // Bytes of one vector.
 __host__ __device__ inline uint32_t param_bytes(bool shared, int threads, int nv) { return (uint32_t)(shared ? threads : kThreads) * nv * 32; }
-// w_post and b_post, a channel gate multiplied in (gate (hat w + b) = hat (gate w) + gate b).
-template <bool VEC>
+// w_post and b_post, a channel gate multiplied in (gate (hat w + b) = hat (gate w) + gate b); zeros behind column d, so that what they multiply adds
+// nothing to a sum there.
+template <int VEC>
 __device__ __forceinline__ void post_params(const Params& p, int v, int t, int threads, f2* w, f2* b) {
     param8<VEC>(p.w_post, 1.0f, v, t, threads, p.d, w);
     param8<VEC>(p.b_post, 0.0f, v, t, threads, p.d, b);
@@ -352,6 +388,8 @@ __device__ __forceinline__ void post_params(const Params& p, int v, int t, int t
 #pragma unroll
         for (int j = 0; j < 4; ++j) { w[j] = mul2(w[j], g[j]); b[j] = mul2(b[j], g[j]); }
     }
+    cut8<VEC>(v, t, threads, p.d, w);
+    cut8<VEC>(v, t, threads, p.d, b);
 }
 
 Params params_of(const ResNorm& a);

@@ -14,31 +14,34 @@ enum { IN_X = 0, IN_Y, IN_DR, IN_DN, IN_GATE, IN_COUNT };
 
 // Persistent blocks of 512 threads, `threads` of them to a row, 8 NV columns a thread; a thread keeps the column sums of its
 // columns over its rows.  RING: the inputs of the next rows are on their way to shared memory while a row is worked on, parameters stay there, a
-// channel gate is part of them.  Without (rows of more than 4096 columns): everything loaded when it is needed.
+// channel gate is part of them.  Without (rows of more than 4096 columns in fp32, with biases or off 16-byte boundaries): everything loaded when it is
+// needed (4000 rows of 8192 265 us, with 90).
 // GATE (of bigmac_gate_t, kNoBlock, kAnyGate) and DN are fixed at compile time for RING: with the choice at run time a row took twice the
 // instructions.  BIAS: the sums that only biases need are kept, too; without them there is room for 16 columns a thread, and half the threads of a
 // row are a third fewer instructions for it (16384 rows of 4096, RMS norms, a full gate: 219 us with 8 columns, 183 with 16).  There, what is needed again
 // behind a sum is read again from shared memory; with 8 columns it is held in registers (16384 rows of 2048, LayerNorms: 101 us, read again 118).
-template <typename T, int NV, bool VEC, bool RING, int GATE, bool DN, bool BIAS>
+template <typename T, int NV, int VEC, bool RING, int GATE, bool DN, bool BIAS>
 __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Params p, int threads, int stages) {
     extern __shared__ __align__(16) uint8_t smem[];
     constexpr int SB = BIAS ? 4 * NV : 1;
     constexpr bool HOLD = NV == 1;
     constexpr int H = HOLD ? 4 : 1;
-    __shared__ float sums[2][kThreads / 32][32];
+    __shared__ __align__(16) float sums[2][kThreads / 32][32];
     grid_dependency_launch();
     grid_dependency_wait();
     const int t = threadIdx.x % threads, group = threadIdx.x / threads, groups = kThreads / threads;
     const int first = (int)blockIdx.x * groups + group, step = (int)gridDim.x * groups;
     const bool working = group < groups;                               // threads that are no whole row rest
-    Row at{sums[0][working ? group : 0], sums[1][working ? group : 0], t, threads, 1 + group};
+    Row at(sums[0][working ? group : 0], sums[1][working ? group : 0], t, threads, 1 + group);
     const int gate_kind = GATE == kAnyGate ? p.gate_kind : GATE;       // RING: a channel gate counts as none
     const bool has_y = GATE == kAnyGate ? p.y != nullptr : GATE != kNoBlock;
     const bool has_dn = GATE == kAnyGate ? p.dn != nullptr : DN;
-    Ring<T, VEC, IN_COUNT, NV> ring;
-    ring.in[IN_X] = (const T*)p.x; ring.in[IN_Y] = (const T*)p.y; ring.in[IN_DR] = (const T*)p.dr; ring.in[IN_DN] = (const T*)p.dn; ring.in[IN_GATE] = (const T*)p.gate;
-    ring.ld[IN_X] = p.x_ld; ring.ld[IN_Y] = p.y_ld; ring.ld[IN_DR] = p.dr_ld; ring.ld[IN_DN] = p.dn_ld; ring.ld[IN_GATE] = p.gate_ld;
-    ring.has[IN_X] = true; ring.has[IN_Y] = has_y; ring.has[IN_DR] = p.dr != nullptr; ring.has[IN_DN] = has_dn; ring.has[IN_GATE] = gate_kind == BIGMAC_GATE_FULL;
+    constexpr int COUNT = GATE == BIGMAC_GATE_FULL || GATE == kAnyGate ? IN_COUNT : IN_COUNT - 1;
+    Ring<T, VEC, COUNT, NV> ring;
+    ring.in[IN_X] = (const T*)p.x; ring.in[IN_Y] = (const T*)p.y; ring.in[IN_DR] = (const T*)p.dr; ring.in[IN_DN] = (const T*)p.dn;
+    ring.ld[IN_X] = p.x_ld; ring.ld[IN_Y] = p.y_ld; ring.ld[IN_DR] = p.dr_ld; ring.ld[IN_DN] = p.dn_ld;
+    ring.has[IN_X] = true; ring.has[IN_Y] = has_y; ring.has[IN_DR] = p.dr != nullptr; ring.has[IN_DN] = has_dn;
+    if constexpr (COUNT == IN_COUNT) { ring.in[IN_GATE] = (const T*)p.gate; ring.ld[IN_GATE] = p.gate_ld; ring.has[IN_GATE] = gate_kind == BIGMAC_GATE_FULL; }
     auto get = [&](int stage, int which, int v, int row, f2* f) {
         if constexpr (RING) ring.get(stage, which, v, row, t, threads, f);
         else if (ring.has[which]) load8<T, VEC>(row_at(ring.in[which], row, ring.ld[which]), v, t, threads, p.d, f);
@@ -52,7 +55,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Pa
         else param8<VEC>(which == W_POST ? p.w_post : which == W_PRE ? p.w_pre : p.b_post, which == B_POST ? 0.0f : 1.0f, v, t, threads, p.d, f);
     };
     auto gate8 = [&](int stage, int v, int row, float token, f2* f) {
-        if (gate_kind == BIGMAC_GATE_FULL) get(stage, IN_GATE, v, row, f);
+        if (COUNT == IN_COUNT && gate_kind == BIGMAC_GATE_FULL) get(stage, COUNT - 1, v, row, f);
         else if (gate_kind == BIGMAC_GATE_CHANNEL) load8<float, VEC>((const float*)p.gate, v, t, threads, p.d, f);
         else fill8(token, f);
     };
@@ -166,7 +169,7 @@ __global__ void __launch_bounds__(kThreads, 1) residual_norm_bwd_kernel(const Pa
                     param(W_POST, v, w);
                     if (gate_kind != BIGMAC_GATE_NONE) gate8(stage, v, row, token, g);
                 }
-                cut8<VEC>(v, t, threads, p.d, D + 4 * v);
+                if (!RING) cut8<VEC>(v, t, threads, p.d, D + 4 * v);       // RING: w_post and b_post are zeros there
                 if ((gate_kind == BIGMAC_GATE_FULL && p.dgate) || gate_kind == BIGMAC_GATE_TOKEN) {
                     if (BIAS && !HOLD) param(B_POST, v, b); else fill8(0.0f, b);
 #pragma unroll
@@ -274,14 +277,14 @@ __global__ void __launch_bounds__(1024) residual_norm_sums_kernel(const float* _
 
 constexpr size_t kBwdSmem = 214 * 1024;                                // and 4 KB for sums
 
-template <typename T, int NV, bool VEC, bool RING, int GATE, bool DN, bool BIAS>
+template <typename T, int NV, int VEC, bool RING, int GATE, bool DN, bool BIAS>
 cudaError_t backward(const ResNorm& a, float* partial, int grid, cudaStream_t stream) {
     auto kernel = residual_norm_bwd_kernel<T, NV, VEC, RING, GATE, DN, BIAS>;
     const int threads = threads_of(a.q->d, NV), groups = kThreads / threads;
     size_t smem = (size_t)groups * a.q->d * sizeof(float);             // the block's sums at the end
     int stages = 0;
     if (RING) {
-        const size_t stage = stage_bytes(VEC, a.q->d, (int)sizeof(T), groups, IN_COUNT, NV), par = (BIAS ? 3 : 2) * param_bytes(NV == 2, threads, NV);
+        const size_t stage = stage_bytes(VEC, a.q->d, (int)sizeof(T), groups, GATE == BIGMAC_GATE_FULL ? IN_COUNT : IN_COUNT - 1, NV), par = (BIAS ? 3 : 2) * param_bytes(NV == 2, threads, NV);
         stages = (int)((kBwdSmem - par) / stage > 4 ? 4 : (kBwdSmem - par) / stage);
         if (stages < 1) return cudaErrorInvalidValue;
         if (par + stages * stage > smem) smem = par + stages * stage;
@@ -309,7 +312,7 @@ int blocks_of(int T, int d, int nv) {
     const int64_t want = ((int64_t)T + groups - 1) / groups;
     return (int)(want < sms ? want : sms);
 }
-template <typename T, int NV, bool VEC, bool DN, bool BIAS>
+template <typename T, int NV, int VEC, bool DN, bool BIAS>
 cudaError_t backward_by_gate(const ResNorm& a, float* partial, int grid, cudaStream_t stream) {
     if (!a.q->y.p) return backward<T, NV, VEC, true, kNoBlock, DN, BIAS>(a, partial, grid, stream);
     switch (a.q->gate_kind) {
@@ -321,13 +324,13 @@ cudaError_t backward_by_gate(const ResNorm& a, float* partial, int grid, cudaStr
 template <typename T>
 cudaError_t backward_any(const ResNorm& a, float* partial, int grid, cudaStream_t stream) {
     const bool dn = a.q->dn.p != nullptr;
-    if (a.q->d > 8 * kThreads)
-        return a.vec ? backward<T, 2, true, false, kAnyGate, true, true>(a, partial, grid, stream) : backward<T, 2, false, false, kAnyGate, true, true>(a, partial, grid, stream);
+    if (a.q->d > 8 * kThreads && (!a.vec || sizeof(T) == 4 || wants_bias(*a.q)))
+        return a.vec ? backward<T, 2, kVecOf<T>, false, kAnyGate, true, true>(a, partial, grid, stream) : backward<T, 2, kAlternate, false, kAnyGate, true, true>(a, partial, grid, stream);
     if constexpr (sizeof(T) == 2)
         if (bwd_pieces(a) == 2)
-            return dn ? backward_by_gate<T, 2, true, true, false>(a, partial, grid, stream) : backward_by_gate<T, 2, true, false, false>(a, partial, grid, stream);
-    if (a.vec) return dn ? backward_by_gate<T, 1, true, true, true>(a, partial, grid, stream) : backward_by_gate<T, 1, true, false, true>(a, partial, grid, stream);
-    return dn ? backward_by_gate<T, 1, false, true, true>(a, partial, grid, stream) : backward_by_gate<T, 1, false, false, true>(a, partial, grid, stream);
+            return dn ? backward_by_gate<T, 2, kVecOf<T>, true, false>(a, partial, grid, stream) : backward_by_gate<T, 2, kVecOf<T>, false, false>(a, partial, grid, stream);
+    if (a.vec) return dn ? backward_by_gate<T, 1, kVecOf<T>, true, true>(a, partial, grid, stream) : backward_by_gate<T, 1, kVecOf<T>, false, true>(a, partial, grid, stream);
+    return dn ? backward_by_gate<T, 1, kAlternate, true, true>(a, partial, grid, stream) : backward_by_gate<T, 1, kAlternate, false, true>(a, partial, grid, stream);
 }
 
 }  // namespace
