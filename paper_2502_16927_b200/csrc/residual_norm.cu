@@ -88,11 +88,13 @@ __global__ void __launch_bounds__(1024 / NV) residual_norm_kernel(const Params p
     if (p.stats && t == 0) p.stats[row] = st;
 }
 
-// Many rows: persistent blocks of 512 threads, two on an SM, `threads` of them to a row, eight columns a thread.  A block a row spent 2 us
-// of an SM on a row of 4096 columns whatever its type, all of it latencies one after the other (loads, sums, parameters, sums); here the next rows are on
-// their way meanwhile and the parameters stay in shared memory.
-template <typename T, int VEC, int GATE>
-__global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const Params p, int threads, int stages, int vectors) {
+// Many rows: persistent blocks of 512 threads, `threads` of them to a row, 8 NV columns a thread: two blocks on an SM with eight columns, one with 16.  A
+// block a row spent 2 us of an SM on a row of 4096 columns whatever its type, all of it latencies one after the other (loads, sums, parameters,
+// sums); here the next rows are on their way meanwhile and the parameters stay in shared memory (4000 rows of 8192: 100 us a block a row, 53 here).
+template <int NV>
+constexpr bool kSharedParams = NV == 2;                                // 16 columns a thread: a block's rows read one copy, which leaves room for more rows
+template <typename T, int NV, int VEC, int GATE>
+__global__ void __launch_bounds__(kThreads, NV == 1 ? 2 : 1) residual_norm_rows_kernel(const Params p, int threads, int stages, int vectors) {
     extern __shared__ __align__(16) uint8_t smem[];
     constexpr int COUNT = GATE == kNoBlock ? 1 : GATE == BIGMAC_GATE_FULL ? 3 : 2;
     __shared__ __align__(16) float sums[2][kThreads / 32][32];
@@ -102,28 +104,29 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
     if (group >= groups) return;                                       // threads that are no whole row
     const int first = (int)blockIdx.x * groups + group, step = (int)gridDim.x * groups;
     Row at(sums[0][group], sums[1][group], t, threads, 1 + group);
-    Ring<T, VEC, COUNT> ring;
+    Ring<T, VEC, COUNT, NV> ring;
     const void* const in[3] = {p.x, p.y, p.gate};
     const int ld[3] = {p.x_ld, p.y_ld, p.gate_ld};
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) { ring.in[i] = (const T*)in[i]; ring.ld[i] = ld[i]; ring.has[i] = true; }
-    ring.init(smem + vectors * param_bytes(false, threads, 1), group, stages, p);
+    ring.init(smem + vectors * param_bytes(kSharedParams<NV>, threads, NV), group, stages, p);
     ring.template start<VEC>(first, step, t, threads);
     // vectors 0, 1: w and b of the norm before, 2, 3: of the one behind; b only with `vectors` = 4.
-    ParamStore<1, false> par(smem, t, threads);
+    ParamStore<NV, kSharedParams<NV>> par(smem, t, threads);
     const int pre = vectors / 2;
-    {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
         f2 w[4], b[4];
         if (GATE != kNoBlock) {
-            post_params<VEC>(p, 0, t, threads, w, b);
-            par.put(0, 0, w);
-            if (vectors == 4) par.put(1, 0, b);
+            post_params<VEC>(p, v, t, threads, w, b);
+            par.put(0, v, w);
+            if (vectors == 4) par.put(1, v, b);
         }
-        param8<VEC>(p.w_pre, 1.0f, 0, t, threads, p.d, w);
-        par.put(pre, 0, w);
+        param8<VEC>(p.w_pre, 1.0f, v, t, threads, p.d, w);
+        par.put(pre, v, w);
         if (vectors == 4) {
-            param8<VEC>(p.b_pre, 0.0f, 0, t, threads, p.d, b);
-            par.put(3, 0, b);
+            param8<VEC>(p.b_pre, 0.0f, v, t, threads, p.d, b);
+            par.put(3, v, b);
         }
     }
     int stage = 0;
@@ -132,34 +135,47 @@ __global__ void __launch_bounds__(kThreads, 2) residual_norm_rows_kernel(const P
         const float token = GATE == BIGMAC_GATE_TOKEN ? ((const float*)p.gate)[row] : 1.0f;
         if constexpr (VEC) ring.arrived();
         else ring.next(stage, row, step, at);
-        f2 r[4];
+        f2 r[4 * NV];
         float4 st = make_float4(0.0f, 1.0f, 0.0f, 1.0f);
-        ring.get(stage, 0, 0, row, t, threads, r);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = mul2(rho, r[j]);
+        for (int v = 0; v < NV; ++v) ring.get(stage, 0, v, row, t, threads, r + 4 * v);
+#pragma unroll
+        for (int j = 0; j < 4 * NV; ++j) r[j] = mul2(rho, r[j]);
         if constexpr (GATE != kNoBlock) {
-            f2 y[4], w[4], b[4], g[4];
-            ring.get(stage, 1, 0, row, t, threads, y);
-            if constexpr (GATE == BIGMAC_GATE_FULL) ring.get(stage, 2, 0, row, t, threads, g);
-            row_stats<1, VEC>(p.post, y, p.post_eps, p, at, st.x, st.y);
-            par.get(0, 0, w);
-            if (vectors == 4) par.get(1, 0, b); else fill8(0.0f, b);
+            f2 y[4 * NV];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const f2 a = fma2(mul2(add2(y[j], pk(-st.x)), pk(st.y)), w[j], b[j]);
-                r[j] = GATE == BIGMAC_GATE_FULL ? fma2(g[j], a, r[j]) : GATE == BIGMAC_GATE_TOKEN ? fma2(pk(token), a, r[j]) : add2(a, r[j]);
+            for (int v = 0; v < NV; ++v) ring.get(stage, 1, v, row, t, threads, y + 4 * v);
+            row_stats<NV, VEC>(p.post, y, p.post_eps, p, at, st.x, st.y);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                f2 w[4], b[4], g[4];
+                if constexpr (GATE == BIGMAC_GATE_FULL) ring.get(stage, 2, v, row, t, threads, g);
+                par.get(0, v, w);
+                if (vectors == 4) par.get(1, v, b); else fill8(0.0f, b);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int i = 4 * v + j;
+                    const f2 a = fma2(mul2(add2(y[i], pk(-st.x)), pk(st.y)), w[j], b[j]);
+                    r[i] = GATE == BIGMAC_GATE_FULL ? fma2(g[j], a, r[i]) : GATE == BIGMAC_GATE_TOKEN ? fma2(pk(token), a, r[i]) : add2(a, r[i]);
+                }
             }
         }
         if constexpr (VEC) ring.again(stage, row, step, at);
-        if (p.r) store8<T, VEC>(row_at((T*)p.r, row, p.r_ld), 0, t, threads, p.d, r);
-        if (p.n) {
-            f2 w[4], b[4];
-            row_stats<1, VEC>(p.pre, r, p.pre_eps, p, at, st.z, st.w);
-            par.get(pre, 0, w);
-            if (vectors == 4) par.get(3, 0, b); else fill8(0.0f, b);
+        if (p.r) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = fma2(mul2(add2(r[j], pk(-st.z)), pk(st.w)), w[j], b[j]);
-            store8<T, VEC>(row_at((T*)p.n, row, p.n_ld), 0, t, threads, p.d, w);
+            for (int v = 0; v < NV; ++v) store8<T, VEC>(row_at((T*)p.r, row, p.r_ld), v, t, threads, p.d, r + 4 * v);
+        }
+        if (p.n) {
+            row_stats<NV, VEC>(p.pre, r, p.pre_eps, p, at, st.z, st.w);
+#pragma unroll
+            for (int v = 0; v < NV; ++v) {
+                f2 w[4], b[4];
+                par.get(pre, v, w);
+                if (vectors == 4) par.get(3, v, b); else fill8(0.0f, b);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = fma2(mul2(add2(r[4 * v + j], pk(-st.z)), pk(st.w)), w[j], b[j]);
+                store8<T, VEC>(row_at((T*)p.n, row, p.n_ld), v, t, threads, p.d, w);
+            }
         }
         if (p.stats && t == 0) p.stats[row] = st;
         stage = stage + 1 == stages ? 0 : stage + 1;
@@ -176,40 +192,45 @@ cudaError_t one_row_a_block(const ResNorm& a, cudaStream_t stream) {
 
 constexpr size_t kRowsSmem = 108 * 1024;                               // of a block, two to an SM (and 4 KB for sums)
 
-template <typename T, int VEC, int GATE>
+template <typename T, int NV, int VEC, int GATE>
 cudaError_t persistent(const ResNorm& a, cudaStream_t stream) {
-    auto kernel = residual_norm_rows_kernel<T, VEC, GATE>;
-    const int threads = threads_of(a.q->d, 1), groups = kThreads / threads, count = GATE == kNoBlock ? 1 : GATE == BIGMAC_GATE_FULL ? 3 : 2;
+    auto kernel = residual_norm_rows_kernel<T, NV, VEC, GATE>;
+    const int threads = threads_of(a.q->d, NV), groups = kThreads / threads, count = GATE == kNoBlock ? 1 : GATE == BIGMAC_GATE_FULL ? 3 : 2;
     const int vectors = a.q->b_post || a.q->b_pre ? 4 : 2;
-    const size_t stage = stage_bytes(VEC, a.q->d, (int)sizeof(T), groups, count), par = vectors * param_bytes(false, threads, 1), left = kRowsSmem - par;
+    const size_t stage = stage_bytes(VEC, a.q->d, (int)sizeof(T), groups, count, NV), par = vectors * param_bytes(kSharedParams<NV>, threads, NV), left = (NV == 1 ? 1 : 2) * kRowsSmem - par;
     const int stages = (int)(left / stage < 1 ? 1 : left / stage > 4 ? 4 : left / stage);
     static PerDeviceOnce once;
     int dev;
     if (once.needed(&dev)) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 2 * (int)kRowsSmem);
         if (e != cudaSuccess) return e;
         once.mark(dev);
     }
-    const int64_t want = ((int64_t)a.T + groups - 1) / groups, most = 2 * (int64_t)gemm_tc_sm_count();
+    const int64_t want = ((int64_t)a.T + groups - 1) / groups, most = (NV == 1 ? 2 : 1) * (int64_t)gemm_tc_sm_count();
     return launch_chained(kernel, (int)(want < most ? want : most), kThreads, par + stages * stage, stream, params_of(a), threads, stages, vectors);
 }
-template <typename T, int VEC>
+template <typename T, int NV, int VEC>
 cudaError_t persistent_by_gate(const ResNorm& a, cudaStream_t stream) {
-    if (!a.q->y.p) return persistent<T, VEC, kNoBlock>(a, stream);
+    if (!a.q->y.p) return persistent<T, NV, VEC, kNoBlock>(a, stream);
     switch (a.q->gate_kind) {
-        case BIGMAC_GATE_TOKEN: return persistent<T, VEC, BIGMAC_GATE_TOKEN>(a, stream);
-        case BIGMAC_GATE_FULL: return persistent<T, VEC, BIGMAC_GATE_FULL>(a, stream);
-        default: return persistent<T, VEC, BIGMAC_GATE_NONE>(a, stream);
+        case BIGMAC_GATE_TOKEN: return persistent<T, NV, VEC, BIGMAC_GATE_TOKEN>(a, stream);
+        case BIGMAC_GATE_FULL: return persistent<T, NV, VEC, BIGMAC_GATE_FULL>(a, stream);
+        default: return persistent<T, NV, VEC, BIGMAC_GATE_NONE>(a, stream);
     }
 }
+// Columns a thread of the persistent blocks has, in pieces of eight: 16 are half the threads, and so half the instructions for the sums, of a row (us with
+// eight / 16: 16384 x 4096 RMS, a full gate 114 / 107, 16384 x 2048 LayerNorms 69 / 63, 8000 x 1357 51 / 45, but 8000 x 1104 25.5 / 26.3).
 template <typename T>
 cudaError_t forward(const ResNorm& a, cudaStream_t stream) {
     const int d = a.q->d;
-    const bool wide = d > 8 * kThreads;
-    const int64_t rows_at_once = (int64_t)2 * gemm_tc_sm_count() * (wide ? 1 : kThreads / threads_of(d, 1));
-    if (!wide && a.T > rows_at_once && (sizeof(T) == 2 || !a.vec)) return a.vec ? persistent_by_gate<T, kVecOf<T>>(a, stream) : persistent_by_gate<T, kAlternate>(a, stream);
-    if (!a.vec) return one_row_a_block<T, 2, kAlternate>(a, stream);
-    return wide || (sizeof(T) == 4 && a.T > rows_at_once) ? one_row_a_block<T, 2, kVecOf<T>>(a, stream) : one_row_a_block<T, 1, kVecOf<T>>(a, stream);
+    const bool wide = d > 8 * kThreads, many = a.T > (int64_t)2 * gemm_tc_sm_count() * (wide ? 1 : kThreads / threads_of(d, 1)), pairs = d > 1280;
+    if constexpr (sizeof(T) == 2)
+        if (many && a.vec) return pairs ? persistent_by_gate<T, 2, kNeighbours>(a, stream) : persistent_by_gate<T, 1, kNeighbours>(a, stream);
+    if (!a.vec) {
+        if (!many || wide) return one_row_a_block<T, 2, kAlternate>(a, stream);
+        return pairs ? persistent_by_gate<T, 2, kAlternate>(a, stream) : persistent_by_gate<T, 1, kAlternate>(a, stream);
+    }
+    return wide || (sizeof(T) == 4 && many) ? one_row_a_block<T, 2, kVecOf<T>>(a, stream) : one_row_a_block<T, 1, kVecOf<T>>(a, stream);
 }
 
 }  // namespace

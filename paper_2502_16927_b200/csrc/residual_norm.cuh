@@ -357,7 +357,7 @@ struct Ring {
 };
 
 // Vectors of parameters in shared memory: piece v of vector `which`, 32 bytes in two pieces.  Every thread its own columns, which takes constant
-// offsets (7 % of the forward); SHARED: the rows of a block read the same ones, where there is no room for that.
+// offsets (7 % of the forward with eight columns a thread); SHARED: the rows of a block read one copy, where there is no room for that.
 template <int NV, bool SHARED>
 struct ParamStore {
     uint8_t* base;                                                     // the thread's first piece

@@ -337,3 +337,19 @@ def test_binding_refuses_mismatched_tensors(binding):
     for bad in (None, stats[:3], stats.double()):
         with pytest.raises(ValueError):
             binding.residual_norm_backward(x, x, None, binding.Norm(1), binding.Norm(1), r, n, bad)
+
+
+@pytest.mark.parametrize("T,d", [(310, 4095), (310, 4096), (310, 4097), (310, 8192), (310, 8191), (700, 1281), (700, 1280), (700, 1288)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_many_rows_with_everything(binding, T, d, dtype):
+    """Both LayerNorms with weights and biases and a gate for every element, more rows than are worked on at once: the most shared memory that a
+    row of each layout takes."""
+    _run(binding, T, d, dtype, LAYER, LAYER, 3, seed=d)
+
+
+@pytest.mark.parametrize("T,d", [(310, 8192), (310, 4104), (310, 5000)])
+@pytest.mark.parametrize("gate_kind", [0, 1, 2, 3])
+def test_many_wide_rows_without_parameters(binding, T, d, gate_kind):
+    """No biases: rows of more than 4096 columns through shared memory in the backward, too."""
+    _run(binding, T, d, torch.bfloat16, RMS, RMS, gate_kind, params=False, seed=d)
+    _run(binding, T, d, torch.bfloat16, LAYER, NONE, gate_kind, params=False, seed=d + 1)
