@@ -35,7 +35,7 @@ __device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 d; asm("add.rn.f32x2 %0, %1,
 
 // A row's elements on its threads: thread t has pieces v of eight.  VEC kNeighbours: eight neighbours (a 16-byte access of bf16); kFours: four and
 // four, each a 16-byte access of fp32 next to the other threads' (eight neighbours are two accesses that use half of every 32-byte sector: backward of 8000 rows of
-// 4096 292 us).  kAlternate, for rows off 16-byte boundaries: the threads' elements alternate, so that accesses to single elements are still whole lines.
+// 4096 292 us, in fours 187).  kAlternate, for rows off 16-byte boundaries: the threads' elements alternate, so that accesses to single elements are still whole lines.
 constexpr int kAlternate = 0, kNeighbours = 1, kFours = 2;
 template <typename T>
 constexpr int kVecOf = sizeof(T) == 4 ? kFours : kNeighbours;
