@@ -35,13 +35,14 @@ __device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 d; asm("add.rn.f32x2 %0, %1,
 
 // A row's elements on its threads: thread t has pieces v of eight.  VEC kNeighbours: eight neighbours (a 16-byte access of bf16); kFours: four and
 // four, each a 16-byte access of fp32 next to the other threads' (eight neighbours are two accesses that use half of every 32-byte sector: backward of 8000 rows of
-// 4096 292 us, in fours 187).  kAlternate, for rows off 16-byte boundaries: the threads' elements alternate, so that accesses to single elements are still whole lines.
+// 4096 292 us, in fours 187).  kAlternate, for rows off 16-byte boundaries: the elements of a warp's threads alternate, so that accesses to single
+// elements are still whole lines, at constant distances (8000 rows of 1357 with the elements of a row's threads alternating 44 us and 79 for the backward, so 36 and 71).
 constexpr int kAlternate = 0, kNeighbours = 1, kFours = 2;
 template <typename T>
 constexpr int kVecOf = sizeof(T) == 4 ? kFours : kNeighbours;
 template <int VEC>
 __device__ __forceinline__ int column(int v, int j, int t, int threads) {
-    return VEC == kNeighbours ? (v * threads + t) * 8 + j : VEC == kFours ? (2 * v + (j >> 2)) * 4 * threads + 4 * t + (j & 3) : (v * 8 + j) * threads + t;
+    return VEC == kNeighbours ? (v * threads + t) * 8 + j : VEC == kFours ? (2 * v + (j >> 2)) * 4 * threads + 4 * t + (j & 3) : (v * threads + (t & ~31)) * 8 + 32 * j + (t & 31);
 }
 
 __device__ __forceinline__ f2 pair_of(uint32_t w) { return pk(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
@@ -77,7 +78,7 @@ __device__ __forceinline__ void load8(const T* row, int v, int t, int threads, i
     } else {
         float e[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = c0 + j * threads < d ? to_float(row[c0 + j * threads]) : 0.0f;
+        for (int j = 0; j < 8; ++j) e[j] = c0 + j * 32 < d ? to_float(row[c0 + j * 32]) : 0.0f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) f[j] = pk(e[2 * j], e[2 * j + 1]);
     }
@@ -109,7 +110,7 @@ __device__ __forceinline__ void store8(T* row, int v, int t, int threads, int d,
     } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (c0 + j * threads < d) from_float(e[j], row + c0 + j * threads);
+            if (c0 + j * 32 < d) from_float(e[j], row + c0 + j * 32);
     }
 }
 // Zeros behind column d.
@@ -126,7 +127,7 @@ __device__ __forceinline__ void cut8(int v, int t, int threads, int d, f2* f) {
         for (int j = 0; j < 4; ++j) {
             float a, b;
             upk(f[j], a, b);
-            f[j] = pk(c0 + 2 * j * threads < d ? a : 0.0f, c0 + (2 * j + 1) * threads < d ? b : 0.0f);
+            f[j] = pk(c0 + 64 * j < d ? a : 0.0f, c0 + 64 * j + 32 < d ? b : 0.0f);
         }
     }
 }
@@ -351,7 +352,9 @@ struct Ring {
             }
         } else {
             const T* from = row_at(in[which], row, ld[which]);
-            load8<T, false>(direct(row) ? from : (const T*)(slot(stage, which) + ((uintptr_t)from & 15)), v, t, threads, d, f);
+            // (two loads: through one pointer to either, every element costs a 64-bit address)
+            if (direct(row)) load8<T, kAlternate>(from, v, t, threads, d, f);
+            else load8<T, kAlternate>((const T*)(slot(stage, which) + ((uintptr_t)from & 15)), v, t, threads, d, f);
         }
     }
 };
