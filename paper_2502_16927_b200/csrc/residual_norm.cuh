@@ -77,8 +77,13 @@ __device__ __forceinline__ void load8(const T* row, int v, int t, int threads, i
         }
     } else {
         float e[8];
+        if (c0 + 7 * 32 < d) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) e[j] = c0 + j * 32 < d ? to_float(row[c0 + j * 32]) : 0.0f;
+            for (int j = 0; j < 8; ++j) e[j] = to_float(row[c0 + j * 32]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) e[j] = c0 + j * 32 < d ? to_float(row[c0 + j * 32]) : 0.0f;
+        }
 #pragma unroll
         for (int j = 0; j < 4; ++j) f[j] = pk(e[2 * j], e[2 * j + 1]);
     }
@@ -108,9 +113,14 @@ __device__ __forceinline__ void store8(T* row, int v, int t, int threads, int d,
             *(float4*)(row + c0 + 4) = make_float4(e[4], e[5], e[6], e[7]);
         }
     } else {
+        if (c0 + 7 * 32 < d) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (c0 + j * 32 < d) from_float(e[j], row + c0 + j * 32);
+            for (int j = 0; j < 8; ++j) from_float(e[j], row + c0 + j * 32);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c0 + j * 32 < d) from_float(e[j], row + c0 + j * 32);
+        }
     }
 }
 // Zeros behind column d.
@@ -122,7 +132,7 @@ __device__ __forceinline__ void cut8(int v, int t, int threads, int d, f2* f) {
         if (column<VEC>(v, 4, t, threads) >= d) f[2] = f[3] = pk(0.0f);
     } else if constexpr (VEC) {
         if (c0 >= d) fill8(0.0f, f);
-    } else {
+    } else if (c0 + 7 * 32 >= d) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             float a, b;
