@@ -219,7 +219,7 @@ cudaError_t persistent_by_gate(const ResNorm& a, cudaStream_t stream) {
     }
 }
 // Columns a thread of the persistent blocks has, in pieces of eight: 16 are half the threads, and so half the instructions for the sums, of a row (us with
-// eight / 16: 16384 x 4096 RMS, a full gate 114 / 107, 16384 x 2048 LayerNorms 69 / 63, 8000 x 1357 51 / 45, but 8000 x 1104 25.5 / 26.3).
+// eight / 16: 16384 x 4096 RMS, a full gate 114 / 107, 16384 x 2048 LayerNorms 69 / 63, 8000 x 1357 then 51 / 45, but 8000 x 1104 25.5 / 26.3).
 template <typename T>
 cudaError_t forward(const ResNorm& a, cudaStream_t stream) {
     const int d = a.q->d;

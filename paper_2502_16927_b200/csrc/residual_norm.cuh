@@ -36,7 +36,7 @@ __device__ __forceinline__ f2 add2(f2 a, f2 b) { f2 d; asm("add.rn.f32x2 %0, %1,
 // A row's elements on its threads: thread t has pieces v of eight.  VEC kNeighbours: eight neighbours (a 16-byte access of bf16); kFours: four and
 // four, each a 16-byte access of fp32 next to the other threads' (eight neighbours are two accesses that use half of every 32-byte sector: backward of 8000 rows of
 // 4096 292 us, in fours 187).  kAlternate, for rows off 16-byte boundaries: the elements of a warp's threads alternate, so that accesses to single
-// elements are still whole lines, at constant distances (8000 rows of 1357 with the elements of a row's threads alternating 44 us and 79 for the backward, so 36 and 71).
+// elements are still whole lines, at constant distances (8000 rows of 1357 with the elements of a row's threads alternating 44 us and 79 for the backward, so 34 and 70).
 constexpr int kAlternate = 0, kNeighbours = 1, kFours = 2;
 template <typename T>
 constexpr int kVecOf = sizeof(T) == 4 ? kFours : kNeighbours;

@@ -302,7 +302,7 @@ cudaError_t backward(const ResNorm& a, float* partial, int grid, cudaStream_t st
 }
 // Do the sums that only biases need matter?  (A channel gate's gradient has b_post in it.)
 bool wants_bias(const bigmac_residual_norm_t& q) { return q.b_post || q.db_post || q.db_pre; }
-// Columns a thread has, in pieces of 8.  (Rows off 16-byte boundaries with 16 columns a thread spill registers.)
+// Columns a thread has, in pieces of 8.  (Rows off 16-byte boundaries with 16 columns a thread spill registers: 8000 rows of 2999 158 us, 198.)
 int bwd_pieces(const ResNorm& a) {
     if (a.q->d > 8 * kThreads) return 2;
     return a.vec && !wants_bias(*a.q) && a.q->dtype == BIGMAC_BF16 && a.q->d > 256 ? 2 : 1;
