@@ -833,8 +833,8 @@ class Block:
         if self._kept is None:
             raise RuntimeError("backward needs a training forward first")
         x, n, y, before, after, step = self._kept
-        if step != self.layer._steps:
-            raise RuntimeError("the layer keeps one step: another training forward of it came between")
+        if step != self.layer._steps or self.layer._T != x.shape[0]:   # before the first launch: it writes gradients
+            raise RuntimeError("the layer keeps one step: another forward of it came between")
         own = {name: G[name] for name in ("dw_post", "db_post", "dgate") if name in G}
         dx, dy, _ = residual_norm_backward(x, y, self.gate, self.post, None, dout, None, after, own, self.residual_scale, accumulate, self._gate_kind)
         dn = self.layer.backward(n, dy, W, G, accumulate=accumulate)
