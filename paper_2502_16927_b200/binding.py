@@ -829,12 +829,16 @@ class Block:
 
     def backward(self, dout, W, G, accumulate=False):
         """dx; G: the layer's gradient buffers and, of the block's own parameters, any of dw_pre, db_pre, dw_post, db_post (fp32 [d]) and
-        dgate."""
+        dgate, each a vector of its own (norms that share a parameter, too)."""
         if self._kept is None:
             raise RuntimeError("backward needs a training forward first")
         x, n, y, before, after, step = self._kept
         if step != self.layer._steps or self.layer._T != x.shape[0]:   # before the first launch: it writes gradients
             raise RuntimeError("the layer keeps one step: another forward of it came between")
+        here, vectors = _here(), [(name, G[name]) for name in ("dw_pre", "db_pre", "dw_post", "db_post", "dgate") if G.get(name) is not None]
+        # two calls write them: one would overwrite the other's
+        if len({_vector(t, name, x.shape[1], here) for name, t in vectors}) < len(vectors):
+            raise ValueError("two gradients in one place")
         own = {name: G[name] for name in ("dw_post", "db_post", "dgate") if name in G}
         dx, dy, _ = residual_norm_backward(x, y, self.gate, self.post, None, dout, None, after, own, self.residual_scale, accumulate, self._gate_kind)
         dn = self.layer.backward(n, dy, W, G, accumulate=accumulate)
