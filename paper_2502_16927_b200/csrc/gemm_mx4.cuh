@@ -90,6 +90,60 @@ __device__ __forceinline__ void gelu_chunk(float* v) {
     }
 }
 
+// GELU of 32 accumulators for an output in fp32: as above with q = exp(-z^2 / 2) G(|z|), G(x) = erfcx(x / sqrt 2) / 2 as a polynomial in t = 1 / (1 + 0.3 x), its
+// minimax fit in relative error (5.7e-8) on [0, 13.3].  Off by four units of 2^-23 near 0 and, with the exponent's rounding, by z^2 / 2 of them far
+// from it.  (1 + erf, whose negative tail is a difference of two numbers near 1, is off by 6e-8 of |z| whatever the value: a tenth of it at z = -5.)
+__device__ __forceinline__ void gelu_chunk_f32(float* v) {
+    constexpr float kC[9] = {6.6862244239018764e-06f, 0.11949588358402252f, 0.121862031519413f, 0.0949108824133873f, 0.1420028954744339f,
+                             -0.07573675364255905f, 0.22798816859722137f, -0.16884131729602814f, 0.03831155598163605f};
+    constexpr int kG = 4;
+#pragma unroll
+    for (int g = 0; g < 16; g += kG) {
+        f32x2_t x[kG], t[kG], P[kG];
+#pragma unroll
+        for (int i = 0; i < kG; ++i) {
+            x[i] = pk2(fabsf(v[2 * (g + i)]), fabsf(v[2 * (g + i) + 1]));
+            float d0, d1;
+            upk2(fma2(x[i], pk2(0.3f, 0.3f), pk2(1.0f, 1.0f)), d0, d1);
+            t[i] = pk2(fast_rcp(d0), fast_rcp(d1));
+            P[i] = fma2(pk2(kC[8], kC[8]), t[i], pk2(kC[7], kC[7]));
+        }
+#pragma unroll
+        for (int k = 6; k >= 0; --k)
+#pragma unroll
+            for (int i = 0; i < kG; ++i) P[i] = fma2(P[i], t[i], pk2(kC[k], kC[k]));
+#pragma unroll
+        for (int i = 0; i < kG; ++i) {
+            float &z0 = v[2 * (g + i)], &z1 = v[2 * (g + i) + 1], e0, e1, q0, q1;
+            upk2(mul2(mul2(x[i], pk2(-0.72134752044448170f, -0.72134752044448170f)), x[i]), e0, e1);
+            upk2(mul2(pk2(fast_ex2(e0), fast_ex2(e1)), P[i]), q0, q1);
+            upk2(mul2(x[i], pk2((z0 > 0.0f ? 1.0f : 0.0f) - q0, (z1 > 0.0f ? 1.0f : 0.0f) - q1)), z0, z1);
+        }
+    }
+}
+// GELU's tanh form, z (1 + tanh w) / 2 = z / (1 + exp(-2 w)), which has no such difference; -2 w / ln 2 = z (a + b z^2).
+__device__ __forceinline__ void gelu_tanh_chunk(float* v) {
+    constexpr float kA = -2.3022081986f, kB = -0.1029432396f;             // -2 sqrt(2 / pi) / ln 2, and 0.044715 of it
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const f32x2_t z = pk2(v[2 * i], v[2 * i + 1]);
+        float e0, e1;
+        upk2(mul2(z, fma2(mul2(z, z), pk2(kB, kB), pk2(kA, kA))), e0, e1);
+        upk2(mul2(z, pk2(fast_rcp(1.0f + fast_ex2(e0)), fast_rcp(1.0f + fast_ex2(e1)))), v[2 * i], v[2 * i + 1]);
+    }
+}
+// The activation of a chunk, chosen once for 32 elements (for each of them: ReLU of 131072 x 1024 bf16 results 90 us, so 54); the erf form of narrow results
+// has kernels of its own.
+template <bool ERF>
+__device__ __forceinline__ void act_chunk(int act, float* v) {
+    if (ERF && act == BIGMAC_ACT_GELU_ERF) gelu_chunk_f32(v);
+    else if (act == BIGMAC_ACT_GELU_TANH) gelu_tanh_chunk(v);
+    else if (act == BIGMAC_ACT_RELU) {
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = act_apply(BIGMAC_ACT_RELU, v[i]);
+    }
+}
+
 // The tiles of a walker: t, t + step, ...  All columns of a row tile follow each other (its codes stay in L2).
 struct Mx4Walk {
     int mt, nt, e, step_m, step_n, tiles_n;
@@ -190,9 +244,8 @@ struct Mx4Epilogue {
         if (col0 >= p.N || rows <= 0) return;              // nothing of the tile is here: a warp's 32 rows may lie behind a segment's last
         if (OUT == OUT_BF16_GELU || OUT == OUT_MX4_GELU) {
             gelu_chunk(v);
-        } else if (OUT == OUT_BF16_ACT || ((OUT == OUT_F32 || OUT == OUT_MX4) && p.act != BIGMAC_ACT_IDENTITY)) {
-#pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = act_apply(p.act, v[i]);
+        } else if (OUT != OUT_BF16 && p.act != BIGMAC_ACT_IDENTITY) {
+            act_chunk<OUT == OUT_F32>(p.act, v);
         }
         if constexpr (is_mx4_out(OUT)) {
             if (lane < rows) store_block(p, v, a_row0 + lane, col0 / 32);
