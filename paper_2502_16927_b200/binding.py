@@ -762,8 +762,18 @@ class Layer:
         bigmac_route(self.handle, x, T, W, R, self._scratch)
         return R
 
+    def _check_tokens(self, t, name):
+        """The kernels take a handle's width and type for granted: anything else would be read, or written, past its end."""
+        if t.dim() != 2 or t.shape[1] != self.cfg["d"] or t.dtype is not self.tdtype:
+            raise ValueError(f"{name}: [T, {self.cfg['d']}] of {self.tdtype} is needed, not {tuple(t.shape)} of {t.dtype}")
+
     def _forward_mx4(self, x, W, y, want_routing):
         """The inference forward with experts in 4 bits."""
+        self._check_tokens(x, "x")
+        if y is not None:
+            self._check_tokens(y, "y")
+            if y.shape != x.shape:
+                raise ValueError(f"y has shape {tuple(y.shape)}, not {tuple(x.shape)}")
         T = x.shape[0]
         need = self._need.get((T, "mx4"))
         if need is None:
@@ -820,6 +830,7 @@ class Block:
         self._kept = None
 
     def forward(self, x, W, training=False, want_routing=False):
+        self.layer._check_tokens(x, "x")
         _, n, before = residual_norm_forward(x, pre=self.pre, training=training, want_r=False)
         y = self.layer.forward(n, W, training=training, want_routing=want_routing)
         y, R = y if want_routing else (y, None)
