@@ -825,6 +825,8 @@ class Block:
     the training forward whose gradients it gives: the layer keeps one step."""
 
     def __init__(self, layer: Layer, pre: Norm, post: Optional[Norm] = None, gate: Optional[torch.Tensor] = None, residual_scale: float = 1.0):
+        if pre is None or pre.kind == BIGMAC_NORM_NONE:
+            raise ValueError("pre: a block begins with a norm")
         self.layer, self.pre, self.post, self.gate, self.residual_scale = layer, pre, post, gate, residual_scale
         self._gate_kind = None if gate is None else BIGMAC_GATE_CHANNEL
         self._kept = None

@@ -40,3 +40,9 @@ def test_block(monkeypatch, x, training):
     monkeypatch.setattr(binding, "residual_norm_forward", lambda x, *a, **k: (None, x, None))
     with pytest.raises(ValueError):
         binding.Block(_layer(), binding.Norm(binding.BIGMAC_NORM_RMS)).forward(x, {}, training=training)
+
+
+@pytest.mark.parametrize("pre", [None, binding.Norm(binding.BIGMAC_NORM_NONE)])
+def test_block_without_a_norm_before(pre):
+    with pytest.raises(ValueError):
+        binding.Block(_layer(), pre)
