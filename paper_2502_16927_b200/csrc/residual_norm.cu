@@ -10,7 +10,7 @@
 //
 // All in fp32; r goes into its norm as it is before it is rounded to the output's type, and the backward pass computes it again from x and y (no
 // more bytes than reading r, and exact).  Bound by memory: forward x, y (and a full gate) in, r, n out; backward x, y, dr, dn in,
-// dx, dy out.  Both read every tensor once: a row lies in the registers of one to 32 warps, which share its sums.
+// dx, dy out.  Both read every tensor once: a row lies in the registers of one to 16 warps, which share its sums.
 #include "residual_norm.cuh"
 
 namespace bigmac {
@@ -19,10 +19,10 @@ using namespace resnorm;
 
 namespace {
 
-// Few rows, or rows of more than 4096 columns: one row to `threads` threads, 8 NV columns each.  Rows of a warp may share a block,
-// longer ones have one for themselves.
+// Few rows, fp32 ones on 16-byte boundaries however many, and rows of more than 4096 columns off them: one row to `threads` threads, 8 NV columns
+// each.  Rows of a warp may share a block, longer ones have one for themselves.
 template <typename T, int NV, int VEC>
-__global__ void __launch_bounds__(1024 / NV) residual_norm_kernel(const Params p, int threads) {
+__global__ void __launch_bounds__(kThreads, NV == 1 ? 2 : 1) residual_norm_kernel(const Params p, int threads) {
     __shared__ __align__(16) float sums[2][32];
     grid_dependency_launch();
     grid_dependency_wait();
@@ -186,6 +186,7 @@ __global__ void __launch_bounds__(kThreads, NV == 1 ? 2 : 1) residual_norm_rows_
 template <typename T, int NV, int VEC>
 cudaError_t one_row_a_block(const ResNorm& a, cudaStream_t stream) {
     const int threads = threads_of(a.q->d, NV), rows = threads == 32 ? (a.T < 8 * gemm_tc_sm_count() ? 1 : 8) : 1;
+    if (threads > kThreads) return cudaErrorInvalidValue;             // the room for a row's sums is 16 warps'
     const int64_t grid = ((int64_t)a.T + rows - 1) / rows;
     return launch_chained(residual_norm_kernel<T, NV, VEC>, (int)grid, rows * threads, 0, stream, params_of(a), threads);
 }

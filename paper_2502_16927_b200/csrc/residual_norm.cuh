@@ -410,7 +410,8 @@ __device__ __forceinline__ void post_params(const Params& p, int v, int t, int t
 }
 
 Params params_of(const ResNorm& a);
-// Threads of a row of d columns, 8 nv of them each: whole warps.
+// Threads of a row of d columns, 8 nv of them each: whole warps, kThreads at most.
+static_assert(kResNormMaxWidth <= 16 * kThreads, "16 columns a thread at most: a row's warps have 16 places for their sums");
 inline int threads_of(int d, int nv) { return (d + 8 * nv * 32 - 1) / (8 * nv * 32) * 32; }
 
 }  // namespace resnorm
