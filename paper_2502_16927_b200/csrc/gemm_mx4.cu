@@ -23,8 +23,7 @@ namespace {
 template <int BN, int STAGES>
 struct Mx4Smem {
     static constexpr uint32_t kBBytes = BN * 128;
-    static constexpr int kWTiles = BN > 128 ? BN / 128 : 1;              // row tiles of W's scale bytes
-    static constexpr uint32_t kSfBytes = 2 * kSfTile * (1 + kWTiles);    // A's two k tiles, then W's
+    static constexpr uint32_t kSfBytes = 2 * kSfTile * 2;                // two k tiles of A's row tile, then of W's
     static constexpr uint32_t kStage = kABytes + kBBytes + kSfBytes;     // a multiple of 1024
     static_assert(kStage % 1024 == 0, "128-byte swizzle: stages on 1024-byte boundaries");
     static constexpr int kCols = BN / 2;                                 // columns of an epilogue warp
@@ -39,7 +38,7 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const __grid_constant__ CUtensorMap map_c, const Mx4Params p) {
     using S = Mx4Smem<BN, STAGES>;
     constexpr uint32_t kSfCol = 2 * BN;                                  // scale bytes behind them: A's 8 columns, then W's
-    constexpr uint32_t kTmemCols = kSfCol + 8 + 8 * S::kWTiles <= 256 ? 256 : 512;
+    constexpr uint32_t kTmemCols = kSfCol + 16 <= 256 ? 256 : 512;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = (uint8_t*)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     uint8_t* boxes_c = smem + STAGES * S::kStage;
@@ -96,21 +95,19 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const int a_row = walk.mt * kMx4Tile, n0 = walk.nt * BN, wt = n0 / 128;
                 const uint8_t* sa = p.sa + (int64_t)walk.mt * ktiles * kSfTile;
                 const uint8_t* sw = p.sw + ((int64_t)q.expert * w_row_tiles + wt) * ktiles * kSfTile;
-                const int w_tiles = min(S::kWTiles, w_row_tiles - wt);
                 const int boxes = (q.rows + p.box_rows - 1) / p.box_rows;
                 const uint32_t a_bytes = boxes * p.box_rows * 128;
                 for (int kb = 0; kb < num_kb; ++kb, s = (s + 1 == STAGES ? 0 : s + 1), phase ^= (s == 0)) {
                     mbar_wait_lean(&empty_bar[s], phase, dead, p.status);
                     const uint32_t sf = kSfTile * min(2, ktiles - 2 * kb);
-                    mbar_expect_tx(&full_bar[s], a_bytes + S::kBBytes + sf * (1 + w_tiles));
+                    mbar_expect_tx(&full_bar[s], a_bytes + S::kBBytes + 2 * sf);
                     uint8_t* a = smem + s * S::kStage;
                     uint8_t* b = a + kABytes;
                     uint8_t* f = b + S::kBBytes;
                     for (int i = 0; i < boxes; ++i) tma_load_2d(a + i * p.box_rows * 128, &map_a, &full_bar[s], kb * 128, a_row + i * p.box_rows);
                     tma_load_2d(b, &map_w, &full_bar[s], kb * 128, q.expert * p.N + n0);
                     bulk_load(f, sa + kb * 2 * kSfTile, sf, &full_bar[s]);
-                    for (int i = 0; i < w_tiles; ++i)
-                        bulk_load(f + 2 * kSfTile * (1 + i), sw + ((int64_t)i * ktiles + kb * 2) * kSfTile, sf, &full_bar[s]);
+                    bulk_load(f + 2 * kSfTile, sw + kb * 2 * kSfTile, sf, &full_bar[s]);
                 }
             }
         }
@@ -137,14 +134,12 @@ gemm_mx4_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                     for (int j = 0; j < 2; ++j) {
                         if (j * 128 >= cols) break;
                         copy_scales(fa + 4 * j, df + j * (kSfTile >> 4));
-#pragma unroll
-                        for (int i = 0; i < S::kWTiles; ++i)
-                            copy_scales(fw + 4 * (j * S::kWTiles + i), df + ((2 * (1 + i) + j) * (kSfTile >> 4)));
+                        copy_scales(fw + 4 * j, df + (2 + j) * (kSfTile >> 4));
                     }
 #pragma unroll
                     for (int kk = 0; kk < kSliceK / 64; ++kk) {
                         if (kk * 64 >= cols) break;
-                        umma_mx4(d, da + kk * 2, db + kk * 2, instr_desc_mx4(BN, kk & 1), fa + 4 * (kk >> 1), fw + 4 * S::kWTiles * (kk >> 1) + shift,
+                        umma_mx4(d, da + kk * 2, db + kk * 2, instr_desc_mx4(BN, kk & 1), fa + 4 * (kk >> 1), fw + 4 * (kk >> 1) + shift,
                                  kb != 0 || kk != 0);
                     }
                     umma_commit(&empty_bar[stage]);
