@@ -369,7 +369,7 @@ typedef struct {
 /* Bytes of codes and scales of a matrix (E = 0), of E stacked ones (grouped = 0) or of a grouped one. */
 int bigmac_mx4_bytes(int32_t rows, int32_t K, int32_t E, int grouped, size_t *code_bytes, size_t *scale_bytes);
 
-/* Rows of x [x_rows, K] (dtype; rows ld elements apart, ld * element size a multiple of 16) to 4 bits.  The scale of a block is
+/* Rows of x [x_rows, K] (dtype; 16-byte aligned, rows ld elements apart, ld * element size a multiple of 16) to 4 bits.  The scale of a block is
  * 2^(floor(log2 m) - 2), m its largest magnitude (not below 2^-127), each element the nearest of the representable
  * values, ties to the even code, magnitudes above 6 scales to 6.  A block that holds an infinity or a NaN gets the scale NaN.
  * Row i of `out` is row i of x or, with slot_of_row (device, [rows]), row slot_of_row[i] / k, zeros where that is
@@ -380,8 +380,11 @@ int bigmac_mx4_quantize(const void *x, int32_t dtype, int32_t x_rows, int64_t ld
  * overflow.  Grouped: in the caller's order; rows in no segment are left as they are. */
 int bigmac_mx4_dequantize(const bigmac_mx4_t *q, void *y, int32_t dtype, int64_t ld, void *stream);
 /* c [rows, N] = act(a w^T), act a bigmac_act_t, products and sums in fp32 on the tensor cores, rounded once to dtype; w one
- * matrix of N = w->rows rows, or, for a grouped a, the a->E = w->E matrices of its experts.  c has a->rows rows in
- * the caller's order, ldc elements apart; rows in no segment are left as they are. */
+ * matrix of N = w->rows rows, or, for a grouped a, the a->E = w->E matrices of its experts.  c (16-byte aligned) has a->rows rows in
+ * the caller's order, ldc elements apart; rows in no segment are left as they are.
+ * Both GELUs are evaluated without loss in their negative tails: of a sum z, relative to the value, GELU_ERF to 2^-23 (8 + z^2) for an fp32
+ * result and to 1.2e-5 up to |z| = 5 and 1.3e-4 behind it for one in bf16 or 4 bits, GELU_TANH to 2^-23 (4 + 6 |w|), w the tanh's argument;
+ * factors of |z| below 2^-126 become 0. */
 int bigmac_mx4_matmul(const bigmac_mx4_t *a, const bigmac_mx4_t *w, int32_t act, int32_t dtype, void *c, int64_t ldc,
                       void *stream);
 /* The same with a result in 4 bits, quantised as by bigmac_mx4_quantize from the fp32 values (not rounded to bf16 first): out
