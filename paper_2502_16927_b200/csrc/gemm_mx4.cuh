@@ -61,7 +61,7 @@ __host__ __device__ constexpr uint32_t instr_desc_mx4(int bn, int half) {
 // log2 Phi(-x) on [0, 14] (linear program on Chebyshev nodes, the error behind 8 allowed to be ten times that up to 5), of odd degree with a negative
 // leading coefficient: behind 14 it falls on to minus infinity, so q is 0 there without a look at the argument.  An error of P is a relative
 // one of q, so the negative tail, whose values are the scales and codes of 4-bit blocks that hold nothing else, is as good as the rest: evaluated in fp32, z Phi(z) is off
-// by 1.0e-5 of itself up to |z| = 5 and by 1.1e-4 behind it, of a bf16 half step of 2^-9 to 2^-8; q below 2^-126 (z < -13) becomes 0.  Infinities are
+// by 1.0e-5 of itself up to |z| = 5 and by 1.1e-4 behind it (a bf16 half step is 2^-9 to 2^-8); q below 2^-126 (z < -13) becomes 0.  Infinities are
 // those of the definition: z = inf gives inf, -inf the product with 0, a NaN.  131072 rows of r 256, h 1024: 82.5 us; without an activation 54; with a saturating
 // polynomial for Phi itself, which is off by up to 3.7e-5 whatever the size of the value (a fifth of it at z = -4, all of it from -4.3 on), 78; erff 142.
 __device__ __forceinline__ void gelu_chunk(float* v) {
